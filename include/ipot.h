@@ -304,6 +304,79 @@ int ipot_enable_rope(ipot_t *pot, const void *cos_table, const void *sin_table, 
 int ipot_view_rope(ipot_t *pot, void **K_rot);
 
 /*
+ * Rotary positions for the rows that are not in the pot: a model's queries, and a chunk's keys.
+ *
+ * ipot_rope_tables writes the tables of cosines and sines that ipot_enable_rope and ipot_rope_rows read, for positions
+ * first .. first + n - 1: entry (p, i) is magnitude * cos((first + p) f_i) (sin), i < rotary_dim / 2.  With
+ * t_i = base^(-2 i / rotary_dim), s = factor and L = original_len, the frequencies f_i are
+ *   IPOT_ROPE_PLAIN      t_i
+ *   IPOT_ROPE_LINEAR     t_i / s                      (positions brought back into the trained range)
+ *   IPOT_ROPE_STRETCHED  those of base * s^(r / (r - 2)), r = rotary_dim: the slowest pair turns s times slower, the fastest as before
+ *   IPOT_ROPE_BANDS      by wavelength: pairs that turn more than `high` times in L positions as they are, fewer than `low`
+ *                        times divided by s, between the two a blend that is linear in the number of turns
+ *   IPOT_ROPE_RAMP       a blend that is linear in i: t_i up to pair floor(D(high)), t_i / s from pair ceil(D(low)) on, where
+ *                        D(b) = r ln(L / (2 pi b)) / (2 ln base) is the pair that turns b times in L positions
+ *                        (both limited to 0 .. r - 1).  Its magnitude, where 0 is given, is 0.1 ln(s) + 1; of all others 1.
+ * Angles are taken in 64 bits and reduced there; cosine and sine are fp32, rounded once to the table's type.
+ *   cos_table, sin_table : device, [n][rotary_dim / 2] of type dtype (IPOT_BF16 or IPOT_F32), 16-byte aligned
+ *   cuda_stream          : cudaStream_t of the current device (NULL = the default stream); the call only queues work
+ * No pot is involved.  Errors: INVALID (NULL, misaligned; rotary_dim odd, < 2 or > 256; n < 1; first < 0 or first + n > 2^31;
+ * base <= 1, factor <= 0, magnitude < 0 or one of them not finite; BANDS and RAMP: L <= 0, low <= 0 or high <= low; STRETCHED:
+ * rotary_dim 2), CUDA.
+ */
+enum {
+    IPOT_ROPE_PLAIN = 0,
+    IPOT_ROPE_LINEAR = 1,
+    IPOT_ROPE_STRETCHED = 2,
+    IPOT_ROPE_BANDS = 3,
+    IPOT_ROPE_RAMP = 4
+};
+typedef struct {
+    int rotary_dim;      /* rotated channels of a head, from channel 0 on */
+    int scaling;         /* IPOT_ROPE_PLAIN .. IPOT_ROPE_RAMP */
+    double base;
+    double factor;       /* s; PLAIN ignores it */
+    double original_len; /* L; BANDS and RAMP */
+    double low, high;    /* turns; BANDS and RAMP */
+    double magnitude;    /* 0 = the scaling's own */
+} ipot_rope_spec_t;
+int ipot_rope_tables(const ipot_rope_spec_t *spec, long long first, int n, int dtype, void *cos_table, void *sin_table,
+                     void *cuda_stream);
+
+/*
+ * Where the rows of a [layers][batch][heads][n_tokens][d] array lie: elements between neighbours in each of the first four
+ * indices; the d channels of a row are contiguous.  A NULL pointer to one means dense in that order.  Every stride is
+ * >= 0 and a multiple of 16 bytes.  (An input may repeat rows by a stride of 0; an output's rows must not overlap.)
+ */
+typedef struct {
+    long long layer, stream, head, token;
+} ipot_strides_t;
+
+/*
+ * Rotates a chunk's queries and / or keys at their positions, one call per layer of a model's forward (layers = 1) or for
+ * several.  Token t of stream b has position positions[b][t] (device int32 [batch][n_tokens]) or, if positions is NULL,
+ * first + t.  A negative position marks padding: its rows are left as they are in the output.  A position >= the table's
+ * rows leaves them alone too and raises the sticky status IPOT_E_BOUNDS.  Channels behind rotary_dim are copied.  The rotation is that of
+ * ipot_enable_rope (single precision, rounded once), so keys rotated here at the slots they will have equal the pot's rotated copy
+ * if the tables are the same.
+ *   q, q_out : device, [layers][batch][Hq][n_tokens][d] in the pot's dtype, 16-byte aligned; both NULL: no queries
+ *   k, k_out : the same with Hkv heads; both NULL: no keys
+ *   rope     : the tables [rows][rotary_dim / 2], 16-byte aligned, of type dtype (need not be the pot's); pairing as for
+ *              ipot_enable_rope, within the first rotary_dim channels
+ * In place (q_out == q with equal strides) is allowed; other overlaps of inputs and outputs are not.  `layers` is that of the arrays,
+ * any number up to 65535.  Asynchronous on the pot's stream; the pot's contents are neither read nor changed.
+ * Errors: INVALID (NULL, misaligned, sizes, strides, rotary_dim odd, < 2 or > d, first outside the table, in place with other strides;
+ * n_tokens so large that a stream's work items pass 2^31), CUDA.
+ */
+typedef struct {
+    const void *cos_table, *sin_table;
+    int rows, rotary_dim, pairing, dtype;
+} ipot_rope_t;
+int ipot_rope_rows(ipot_t *pot, const ipot_rope_t *rope, int layers, int n_tokens, const int32_t *positions, int first,
+                   const void *q, const ipot_strides_t *q_strides, void *q_out, const ipot_strides_t *q_out_strides,
+                   const void *k, const ipot_strides_t *k_strides, void *k_out, const ipot_strides_t *k_out_strides);
+
+/*
  * Borrowed device pointers to the pot ([layers][batch][Hkv][pot_size][d]) and
  * the current fill.  Rows >= len are undefined.  The pointers stay valid until
  * ipot_destroy(); their contents are final once the stream's queued work ran.

@@ -8,15 +8,15 @@ import subprocess
 _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
 LIB = os.path.join(_PKG, "libipot.so")
-_SRC = os.path.join(_PKG, "csrc", "ipot_api.cu")
+_SRC = [os.path.join(_PKG, "csrc", "ipot_api.cu"), os.path.join(_PKG, "csrc", "ops.cu")]
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-shared", "-Xcompiler", "-fPIC", "-cudart", "static"]
+              "-shared", "-Xcompiler", "-fPIC", "-cudart", "static", "--threads", "0"]
 
 
 def _sources():
     return (glob.glob(os.path.join(_PKG, "csrc", "*.cu")) + glob.glob(os.path.join(_PKG, "csrc", "*.cuh"))
-            + [os.path.join(_ROOT, "include", "ipot.h")])
+            + glob.glob(os.path.join(_PKG, "csrc", "*.h")) + [os.path.join(_ROOT, "include", "ipot.h")])
 
 
 def stale() -> bool:
@@ -30,7 +30,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
     """Compile the library if it is missing or older than its sources."""
     if force or stale():
         nvcc = os.environ.get("NVCC", "nvcc")
-        cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", LIB, _SRC]
+        cmd = [nvcc] + NVCC_FLAGS + (["-Xptxas", "-v"] if verbose else []) + ["-o", LIB] + _SRC
         subprocess.check_call(cmd)
     return LIB
 

@@ -23,6 +23,7 @@
 #include "k_score_ts.cuh"
 #include "k_score_tw.cuh"
 #include "k_select.cuh"
+#include "ops.h"
 
 using namespace ipotk;
 
@@ -549,6 +550,79 @@ int decode_splits(int units, int slots)
     return best;
 }
 
+namespace {
+// The pot's device for the length of a call: the default stream and a kernel's launch mean the current one.
+struct DeviceGuard {
+    int before = -1;
+    bool ok = true;
+    explicit DeviceGuard(int device)
+    {
+        int now = -1;
+        ok = cudaGetDevice(&now) == cudaSuccess;
+        if (ok && now != device) {
+            ok = cudaSetDevice(device) == cudaSuccess;
+            if (ok) before = now;
+        }
+        if (!ok) cudaGetLastError();
+    }
+    ~DeviceGuard()
+    {
+        if (before >= 0) cudaSetDevice(before);
+    }
+};
+
+// The strides of a [layers][batch][heads][n][d] array of the pot's type; false where they are none the kernels can read 16 bytes at a time.
+bool row_strides(const ipot *p, const ipot_strides_t *s, int heads, int n, Strides &out)
+{
+    const long long d = p->cfg.d;
+    if (!s) {
+        out.token = d;
+        out.head = n * d;
+        out.stream = heads * out.head;
+        out.layer = p->cfg.batch * out.stream;
+        return true;
+    }
+    const int vec = 16 / p->elem_bytes;
+    for (long long v : {s->layer, s->stream, s->head, s->token})
+        if (v < 0 || v % vec || v > (1LL << 40)) return false;
+    out.layer = s->layer; out.stream = s->stream; out.head = s->head; out.token = s->token;
+    return true;
+}
+
+// The frequencies of a table in turns per position; false for a specification that has none.
+bool rope_turns(const ipot_rope_spec_t &c, RopeTableParams &p)
+{
+    const double pi = 3.14159265358979323846;
+    const int r = c.rotary_dim;
+    if (r < 2 || r > 2 * kRopeMaxPairs || r % 2) return false;
+    if (c.scaling < IPOT_ROPE_PLAIN || c.scaling > IPOT_ROPE_RAMP) return false;
+    const bool plain = c.scaling == IPOT_ROPE_PLAIN, parts = c.scaling == IPOT_ROPE_BANDS || c.scaling == IPOT_ROPE_RAMP;
+    const double s = plain ? 1.0 : c.factor, L = c.original_len;
+    if (!(c.base > 1.0) || !(s > 0.0) || !(c.magnitude >= 0.0) || !std::isfinite(c.base) || !std::isfinite(s) || !std::isfinite(c.magnitude)) return false;
+    if (parts && (!(L > 0.0) || !(c.low > 0.0) || !(c.high > c.low) || !std::isfinite(L) || !std::isfinite(c.high))) return false;
+    if (c.scaling == IPOT_ROPE_STRETCHED && r == 2) return false;
+    const double base = c.scaling == IPOT_ROPE_STRETCHED ? c.base * std::pow(s, r / (r - 2.0)) : c.base;
+    if (!(base > 0.0) || !std::isfinite(base)) return false;
+    double lo = 0.0, hi = 0.0;   // RAMP: the pairs between which it blends
+    if (c.scaling == IPOT_ROPE_RAMP) {
+        const double per = r / (2.0 * std::log(base));
+        lo = std::min(std::max(std::floor(per * std::log(L / (2.0 * pi * c.high))), 0.0), r - 1.0);
+        hi = std::max(std::min(std::ceil(per * std::log(L / (2.0 * pi * c.low))), r - 1.0), 0.0);
+    }
+    for (int i = 0; i < r / 2; ++i) {
+        const double t = std::pow(base, -2.0 * i / r);
+        double keep = 1.0;   // how much of t stays; the rest is divided by s
+        if (c.scaling == IPOT_ROPE_LINEAR) keep = 0.0;
+        else if (c.scaling == IPOT_ROPE_BANDS) keep = std::min(1.0, std::max(0.0, (L * t / (2.0 * pi) - c.low) / (c.high - c.low)));
+        else if (c.scaling == IPOT_ROPE_RAMP) keep = 1.0 - std::min(1.0, std::max(0.0, (i - lo) / std::max(hi - lo, 0.001)));
+        p.turns[i] = (keep == 1.0 ? t : keep == 0.0 ? t / s : t * keep + t / s * (1.0 - keep)) / (2.0 * pi);
+    }
+    p.half = r / 2;
+    p.magnitude = (float)(c.magnitude > 0.0 ? c.magnitude : c.scaling == IPOT_ROPE_RAMP ? 0.1 * std::log(s) + 1.0 : 1.0);
+    return true;
+}
+}  // namespace
+
 template <typename T, int G>
 int launch_decode_g(ipot *p, const void *q, float *out, float *lse)
 {
@@ -997,6 +1071,56 @@ int ipot_enable_rope(ipot_t *p, const void *cos_table, const void *sin_table, in
     p->rope_cos = cos_table;
     p->rope_sin = sin_table;
     p->rope = pairing;
+    return IPOT_OK;
+}
+
+int ipot_rope_tables(const ipot_rope_spec_t *spec, long long first, int n, int dtype, void *cos_table, void *sin_table, void *cuda_stream)
+{
+    if (!spec || !cos_table || !sin_table || !aligned16(cos_table) || !aligned16(sin_table)) return IPOT_E_INVALID;
+    if (dtype != IPOT_BF16 && dtype != IPOT_F32) return IPOT_E_INVALID;
+    if (n < 1 || first < 0 || first > (1LL << 31) - n) return IPOT_E_INVALID;
+    RopeTableParams p;
+    if (!rope_turns(*spec, p)) return IPOT_E_INVALID;
+    p.first = first;
+    p.entries = (long long)n * p.half;
+    p.cos_t = cos_table;
+    p.sin_t = sin_table;
+    IPOT_CUDA(launch_rope_tables(p, dtype == IPOT_F32, (cudaStream_t)cuda_stream));
+    return IPOT_OK;
+}
+
+int ipot_rope_rows(ipot_t *p, const ipot_rope_t *rope, int layers, int n, const int32_t *positions, int first, const void *q,
+                   const ipot_strides_t *q_strides, void *q_out, const ipot_strides_t *q_out_strides, const void *k, const ipot_strides_t *k_strides,
+                   void *k_out, const ipot_strides_t *k_out_strides)
+{
+    if (!p || !rope || !rope->cos_table || !rope->sin_table || !aligned16(rope->cos_table) || !aligned16(rope->sin_table)) return IPOT_E_INVALID;
+    if (!q != !q_out || !k != !k_out || (!q && !k)) return IPOT_E_INVALID;
+    if (layers < 1 || layers > 65535 || p->cfg.batch > 65535 || n < 1) return IPOT_E_INVALID;
+    if (rope->dtype != IPOT_BF16 && rope->dtype != IPOT_F32) return IPOT_E_INVALID;
+    if (rope->pairing != IPOT_ROPE_HALF && rope->pairing != IPOT_ROPE_INTERLEAVED) return IPOT_E_INVALID;
+    if (rope->rows < 1 || rope->rotary_dim < 2 || rope->rotary_dim % 2 || rope->rotary_dim > p->cfg.d) return IPOT_E_INVALID;
+    if (reinterpret_cast<uintptr_t>(positions) & 3u) return IPOT_E_INVALID;
+    if (!positions && (first < 0 || first > rope->rows - n)) return IPOT_E_INVALID;
+    RopeRowsParams r;
+    r.src[0] = q; r.src[1] = k; r.dst[0] = q_out; r.dst[1] = k_out;
+    r.heads[0] = q ? p->cfg.Hq : 0;
+    r.heads[1] = k ? p->cfg.Hkv : 0;
+    const ipot_strides_t *in[2] = {q_strides, k_strides}, *out[2] = {q_out_strides, k_out_strides};
+    const int heads[2] = {p->cfg.Hq, p->cfg.Hkv};
+    for (int i = 0; i < 2; ++i) {
+        if (!r.src[i]) continue;
+        if (!aligned16(r.src[i]) || !aligned16(r.dst[i]) || !row_strides(p, in[i], heads[i], n, r.in[i]) || !row_strides(p, out[i], heads[i], n, r.out[i]))
+            return IPOT_E_INVALID;
+        if (r.src[i] == r.dst[i] && memcmp(&r.in[i], &r.out[i], sizeof(Strides))) return IPOT_E_INVALID;
+    }
+    if ((long long)n * p->cfg.d * ((p->cfg.Hq + p->cfg.Hkv + 3) / 4) >= (1LL << 31)) return IPOT_E_INVALID;
+    r.cos_t = rope->cos_table; r.sin_t = rope->sin_table; r.positions = positions;
+    r.first = first; r.table_rows = rope->rows; r.rotary = rope->rotary_dim;
+    r.d = p->cfg.d; r.n = n; r.streams = p->cfg.batch; r.layers = layers; r.status = p->status;
+    DeviceGuard device(p->device);
+    if (!device.ok) return IPOT_E_CUDA;
+    IPOT_CUDA(launch_rope_rows(r, p->cfg.dtype == IPOT_F32, rope->dtype == IPOT_F32, rope->pairing == IPOT_ROPE_INTERLEAVED, p->stream));
+    p->launches += 1;
     return IPOT_OK;
 }
 

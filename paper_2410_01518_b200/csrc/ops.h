@@ -1,0 +1,39 @@
+// Host launchers of the operators around the pot (ops.cu): plain parameters, no pot object.  Arguments have been checked.
+#pragma once
+#include <cuda_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace ipotk {
+
+// Elements between neighbours of a [layer][stream][head][token][d] array; the channels of a row are contiguous.
+struct Strides {
+    long long layer, stream, head, token;
+};
+
+// ------------------------------------------------------------------ rotary positions (k_rotary.cuh)
+constexpr int kRopeMaxPairs = 128;
+struct RopeTableParams {
+    double turns[kRopeMaxPairs];   // of a channel pair per position, in whole turns
+    float magnitude;
+    int half;                      // pairs
+    long long first;
+    long long entries;             // positions * half
+    void *cos_t, *sin_t;
+};
+cudaError_t launch_rope_tables(const RopeTableParams &p, bool f32, cudaStream_t stream);
+
+struct RopeRowsParams {
+    const void *src[2];            // queries, keys; NULL: none of them
+    void *dst[2];
+    Strides in[2], out[2];
+    int heads[2];
+    const void *cos_t, *sin_t;
+    const int32_t *positions;      // [streams][n], or NULL: first + token
+    int first, table_rows, rotary, d, n, streams, layers;
+    int *status;
+};
+// interleaved: pairs (2c, 2c + 1), else (c, c + rotary / 2)
+cudaError_t launch_rope_rows(const RopeRowsParams &p, bool f32, bool table_f32, bool interleaved, cudaStream_t stream);
+
+}  // namespace ipotk

@@ -22,6 +22,7 @@ IPOT_BF16, IPOT_F32 = 0, 1
 IPOT_SCORER_AUTO, IPOT_SCORER_SIMT, IPOT_SCORER_TENSOR, IPOT_SCORER_WARP_MMA, IPOT_SCORER_TENSOR_SWEEPS, IPOT_SCORER_TENSOR_ITEMS = 0, 1, 2, 3, 4, 5
 IPOT_TUNE_SWEEPS_CLUSTER, IPOT_TUNE_SWEEPS_FMA_EIGHTHS, IPOT_TUNE_WAIT_LIMIT_NS, IPOT_TUNE_TEST_WITHHOLD_RANK, IPOT_TUNE_TEST_WITHHOLD_CHUNK = 1, 2, 3, 4, 5
 IPOT_ROPE_HALF, IPOT_ROPE_INTERLEAVED = 1, 2
+IPOT_ROPE_PLAIN, IPOT_ROPE_LINEAR, IPOT_ROPE_STRETCHED, IPOT_ROPE_BANDS, IPOT_ROPE_RAMP = 0, 1, 2, 3, 4
 
 # every symbol include/ipot.h declares
 SYMBOLS = [
@@ -32,7 +33,7 @@ SYMBOLS = [
     "ipot_kernel_ms", "ipot_launch_count", "ipot_strerror", "ipot_cap_scores_noalloc",
     "ipot_score_and_compress_cap", "ipot_score_only_cap", "ipot_score_and_compress_cap_host",
     "ipot_nuc_scores", "ipot_enable_rope", "ipot_view_rope",
-    "ipot_decode_attention", "ipot_set_tuning",
+    "ipot_decode_attention", "ipot_set_tuning", "ipot_rope_tables", "ipot_rope_rows",
 ]
 
 
@@ -40,6 +41,20 @@ class ipot_config_t(C.Structure):
     _fields_ = [("pot_size", C.c_int), ("keep", C.c_int), ("layers", C.c_int), ("Hq", C.c_int),
                 ("Hkv", C.c_int), ("d", C.c_int), ("batch", C.c_int), ("dtype", C.c_int),
                 ("nuc_slots", C.c_int), ("max_cap_rows", C.c_int), ("stream", C.c_void_p)]
+
+
+class ipot_rope_spec_t(C.Structure):
+    _fields_ = [("rotary_dim", C.c_int), ("scaling", C.c_int), ("base", C.c_double), ("factor", C.c_double),
+                ("original_len", C.c_double), ("low", C.c_double), ("high", C.c_double), ("magnitude", C.c_double)]
+
+
+class ipot_strides_t(C.Structure):
+    _fields_ = [("layer", C.c_longlong), ("stream", C.c_longlong), ("head", C.c_longlong), ("token", C.c_longlong)]
+
+
+class ipot_rope_t(C.Structure):
+    _fields_ = [("cos_table", C.c_void_p), ("sin_table", C.c_void_p), ("rows", C.c_int), ("rotary_dim", C.c_int),
+                ("pairing", C.c_int), ("dtype", C.c_int)]
 
 
 class IpotError(RuntimeError):
@@ -85,6 +100,9 @@ def lib() -> C.CDLL:
         L.ipot_decode_attention.argtypes = [vp, vp, vp, vp]
         L.ipot_enable_rope.argtypes = [vp, vp, vp, ip]
         L.ipot_view_rope.argtypes = [vp, C.POINTER(vp)]
+        st = C.POINTER(ipot_strides_t)
+        L.ipot_rope_tables.argtypes = [C.POINTER(ipot_rope_spec_t), C.c_longlong, ip, ip, vp, vp, vp]
+        L.ipot_rope_rows.argtypes = [vp, C.POINTER(ipot_rope_t), ip, ip, vp, ip, vp, st, vp, st, vp, st, vp, st]
         L.ipot_view.argtypes = [vp, C.POINTER(vp), C.POINTER(vp), C.POINTER(ip)]
         L.ipot_last_indices.argtypes = [vp, C.POINTER(vp)]
         L.ipot_last_scores.argtypes = [vp, C.POINTER(vp), C.POINTER(ip)]
@@ -217,6 +235,25 @@ def ipot_view_rope(h) -> int:
     p = C.c_void_p()
     _check(lib().ipot_view_rope(h, C.byref(p)), "ipot_view_rope")
     return p.value
+
+
+def _strides(s):
+    """(layer, stream, head, token) in elements, or None: dense."""
+    return None if s is None else C.byref(ipot_strides_t(*s))
+
+
+def ipot_rope_tables(cos_table, sin_table, first, n, rotary_dim, dtype, base=10000.0, scaling=IPOT_ROPE_PLAIN, factor=1.0,
+                     original_len=0.0, low=0.0, high=0.0, magnitude=0.0, stream=None) -> None:
+    spec = ipot_rope_spec_t(rotary_dim, scaling, base, factor, original_len, low, high, magnitude)
+    _check(lib().ipot_rope_tables(C.byref(spec), first, n, dtype, _ptr(cos_table), _ptr(sin_table), stream), "ipot_rope_tables")
+
+
+def ipot_rope_rows(h, layers, n_tokens, cos_table, sin_table, rows, rotary_dim, pairing, dtype, positions=None, first=0, q=None, q_out=None,
+                   k=None, k_out=None, q_strides=None, q_out_strides=None, k_strides=None, k_out_strides=None) -> None:
+    """Strides: (layer, stream, head, token) in elements, None = dense [layers][batch][heads][n_tokens][d]."""
+    rope = ipot_rope_t(_ptr(cos_table), _ptr(sin_table), rows, rotary_dim, pairing, dtype)
+    _check(lib().ipot_rope_rows(h, C.byref(rope), layers, n_tokens, _ptr(positions), first, _ptr(q), _strides(q_strides), _ptr(q_out),
+                                _strides(q_out_strides), _ptr(k), _strides(k_strides), _ptr(k_out), _strides(k_out_strides)), "ipot_rope_rows")
 
 
 def ipot_view(h):
