@@ -377,6 +377,29 @@ int ipot_rope_rows(ipot_t *pot, const ipot_rope_t *rope, int layers, int n_token
                    const void *k, const ipot_strides_t *k_strides, void *k_out, const ipot_strides_t *k_out_strides);
 
 /*
+ * Attention of a chunk of new tokens, the step of a model's forward that the pot is kept for (Sec. 3.2: a prompt is taken in
+ * chunk by chunk, and each chunk's tokens see the pot and what came before them in the chunk).  For layers layer .. layer +
+ * n_layers - 1 of the pot: token t of query head h attends to rows [0, len) of the unit of KV head h / (Hq / Hkv) and to
+ * the chunk's own rows 0 .. t:  out_h[t] = sum_j softmax_j(q_h[t] . k_j / sqrt(d)) v_j.  The chunk is not in the pot yet
+ * (ipot_append_chunk puts it there when all layers have seen it), and the pot may be empty.  n_tokens = 1 is generation.
+ *   q      : device, [n_layers][batch][Hq][n_tokens][d] in the pot's dtype, 16-byte aligned.  In rotary mode the pot's rows
+ *            that are read are the rotated copy, and q and k are rotated at positions len + t by the caller (ipot_rope_rows).
+ *   k, v   : the same with Hkv heads.
+ *   out    : as q, in the pot's dtype; must not overlap the inputs.
+ *   lse    : device fp32 [n_layers][batch][Hq][n_tokens], or NULL: log sum_j exp(q_h[t] . k_j / sqrt(d)).
+ *   tokens : device int32 [batch], or NULL: how many tokens stream b has (below 0: none, above n_tokens: n_tokens).  The rows of
+ *            out and lse behind them are left as they were, and what lies behind them in q, k and v does not count, whatever it is.
+ * q_strides etc. as for ipot_rope_rows; NULL = dense in the order given.
+ * Logits, softmax and sums are fp32, and in f32 pots everything is.  In bf16 pots the probabilities enter the product with
+ * v as bf16 numbers relative to their row's largest (2^-8 each at most, less than the rounding of the result).
+ * Asynchronous on the pot's stream; the pot is not changed.
+ * Errors: INVALID (NULL, misaligned, sizes, strides; layers outside the pot; n_tokens * (Hq / Hkv) or len + n_tokens beyond 2^30), CUDA.
+ */
+int ipot_chunk_attention(ipot_t *pot, int layer, int n_layers, int n_tokens, const int32_t *tokens, const void *q,
+                         const ipot_strides_t *q_strides, const void *k, const ipot_strides_t *k_strides, const void *v,
+                         const ipot_strides_t *v_strides, void *out, const ipot_strides_t *out_strides, float *lse);
+
+/*
  * Borrowed device pointers to the pot ([layers][batch][Hkv][pot_size][d]) and
  * the current fill.  Rows >= len are undefined.  The pointers stay valid until
  * ipot_destroy(); their contents are final once the stream's queued work ran.

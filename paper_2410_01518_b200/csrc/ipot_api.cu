@@ -1124,6 +1124,32 @@ int ipot_rope_rows(ipot_t *p, const ipot_rope_t *rope, int layers, int n, const 
     return IPOT_OK;
 }
 
+int ipot_chunk_attention(ipot_t *p, int layer, int n_layers, int n, const int32_t *tokens, const void *q, const ipot_strides_t *q_strides, const void *k,
+                         const ipot_strides_t *k_strides, const void *v, const ipot_strides_t *v_strides, void *out, const ipot_strides_t *out_strides, float *lse)
+{
+    if (!p || !q || !k || !v || !out || !aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return IPOT_E_INVALID;
+    if ((reinterpret_cast<uintptr_t>(lse) & 3u) || (reinterpret_cast<uintptr_t>(tokens) & 3u)) return IPOT_E_INVALID;
+    if (layer < 0 || n_layers < 1 || layer > p->cfg.layers - n_layers) return IPOT_E_INVALID;
+    if (n < 1 || n > (1 << 30) - p->cfg.pot_size || (long long)n * p->G > (1 << 30)) return IPOT_E_INVALID;
+    ChunkParams c;
+    if (!row_strides(p, q_strides, p->cfg.Hq, n, c.qs) || !row_strides(p, k_strides, p->cfg.Hkv, n, c.ks) ||
+        !row_strides(p, v_strides, p->cfg.Hkv, n, c.vs) || !row_strides(p, out_strides, p->cfg.Hq, n, c.os))
+        return IPOT_E_INVALID;
+    DeviceGuard device(p->device);
+    if (!device.ok) return IPOT_E_CUDA;
+    int rc = materialise(p, true, true);
+    if (rc != IPOT_OK) return rc;
+    c.q = q; c.k = k; c.v = v; c.out = out; c.lse = lse; c.tokens = tokens;
+    c.potK = score_keys(p); c.potV = p->V;
+    c.unit0 = layer * p->cfg.batch * p->cfg.Hkv;
+    c.unit_rows = p->cfg.pot_size; c.len = p->len;
+    c.layers = n_layers; c.streams = p->cfg.batch; c.Hkv = p->cfg.Hkv; c.G = p->G; c.d = p->cfg.d; c.n = n;
+    c.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)p->cfg.d));
+    IPOT_CUDA(launch_chunk_attention(c, p->cfg.dtype == IPOT_F32, p->stream));
+    p->launches += 1;
+    return IPOT_OK;
+}
+
 int ipot_view_rope(ipot_t *p, void **K_rot)
 {
     if (!p || !K_rot) return IPOT_E_INVALID;

@@ -1,6 +1,7 @@
 // Kernels of the operators around the pot and their launchers: a second compilation unit beside ipot_api.cu.
 #include "ops.h"
 
+#include "k_chunk_fma.cuh"
 #include "k_rotary.cuh"
 
 namespace ipotk {
@@ -21,6 +22,11 @@ cudaError_t launch_rope_rows(const RopeRowsParams &p, bool f32, bool table_f32, 
     }
     if (table_f32) return interleaved ? launch_rope_rows_t<bf16, float, true>(p, stream) : launch_rope_rows_t<bf16, float, false>(p, stream);
     return interleaved ? launch_rope_rows_t<bf16, bf16, true>(p, stream) : launch_rope_rows_t<bf16, bf16, false>(p, stream);
+}
+
+cudaError_t launch_chunk_attention(const ChunkParams &p, bool f32, cudaStream_t stream)
+{
+    return f32 ? launch_chunk_fma<float>(p, stream) : launch_chunk_fma<__nv_bfloat16>(p, stream);
 }
 
 }  // namespace ipotk

@@ -36,4 +36,19 @@ struct RopeRowsParams {
 // interleaved: pairs (2c, 2c + 1), else (c, c + rotary / 2)
 cudaError_t launch_rope_rows(const RopeRowsParams &p, bool f32, bool table_f32, bool interleaved, cudaStream_t stream);
 
+// ------------------------------------------------------------------ a chunk's attention over pot and chunk (k_chunk_*.cuh)
+struct ChunkParams {
+    const void *q, *k, *v;         // of the layers asked for
+    void *out;
+    float *lse;                    // [layers][streams][heads][n], or NULL
+    Strides qs, ks, vs, os;
+    const int32_t *tokens;         // [streams], or NULL: all n
+    const void *potK, *potV;       // [units][unit_rows][d], from the pot's first unit on
+    int unit0;                     // the first unit asked for
+    int unit_rows, len;
+    int layers, streams, Hkv, G, d, n;
+    float scale_log2e;
+};
+cudaError_t launch_chunk_attention(const ChunkParams &p, bool f32, cudaStream_t stream);
+
 }  // namespace ipotk

@@ -34,6 +34,7 @@ SYMBOLS = [
     "ipot_score_and_compress_cap", "ipot_score_only_cap", "ipot_score_and_compress_cap_host",
     "ipot_nuc_scores", "ipot_enable_rope", "ipot_view_rope",
     "ipot_decode_attention", "ipot_set_tuning", "ipot_rope_tables", "ipot_rope_rows",
+    "ipot_chunk_attention",
 ]
 
 
@@ -103,6 +104,7 @@ def lib() -> C.CDLL:
         st = C.POINTER(ipot_strides_t)
         L.ipot_rope_tables.argtypes = [C.POINTER(ipot_rope_spec_t), C.c_longlong, ip, ip, vp, vp, vp]
         L.ipot_rope_rows.argtypes = [vp, C.POINTER(ipot_rope_t), ip, ip, vp, ip, vp, st, vp, st, vp, st, vp, st]
+        L.ipot_chunk_attention.argtypes = [vp, ip, ip, ip, vp, vp, st, vp, st, vp, st, vp, st, vp]
         L.ipot_view.argtypes = [vp, C.POINTER(vp), C.POINTER(vp), C.POINTER(ip)]
         L.ipot_last_indices.argtypes = [vp, C.POINTER(vp)]
         L.ipot_last_scores.argtypes = [vp, C.POINTER(vp), C.POINTER(ip)]
@@ -254,6 +256,12 @@ def ipot_rope_rows(h, layers, n_tokens, cos_table, sin_table, rows, rotary_dim, 
     rope = ipot_rope_t(_ptr(cos_table), _ptr(sin_table), rows, rotary_dim, pairing, dtype)
     _check(lib().ipot_rope_rows(h, C.byref(rope), layers, n_tokens, _ptr(positions), first, _ptr(q), _strides(q_strides), _ptr(q_out),
                                 _strides(q_out_strides), _ptr(k), _strides(k_strides), _ptr(k_out), _strides(k_out_strides)), "ipot_rope_rows")
+
+
+def ipot_chunk_attention(h, layer, n_layers, n_tokens, q, k, v, out, lse=None, tokens=None, q_strides=None, k_strides=None, v_strides=None,
+                         out_strides=None) -> None:
+    _check(lib().ipot_chunk_attention(h, layer, n_layers, n_tokens, _ptr(tokens), _ptr(q), _strides(q_strides), _ptr(k), _strides(k_strides),
+                                      _ptr(v), _strides(v_strides), _ptr(out), _strides(out_strides), _ptr(lse)), "ipot_chunk_attention")
 
 
 def ipot_view(h):
