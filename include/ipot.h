@@ -400,6 +400,38 @@ int ipot_chunk_attention(ipot_t *pot, int layer, int n_layers, int n_tokens, con
                          const ipot_strides_t *v_strides, void *out, const ipot_strides_t *out_strides, float *lse);
 
 /*
+ * Generation over selected blocks of a long pot.  The slots are taken in blocks of block_rows; the library keeps, for every
+ * unit and block, the smallest and the largest value of each key channel (of the rotated copy in rotary mode).  They are
+ * brought up to date by the calls that move rows - ipot_append_chunk(_host) and the cycles, for a deferred append the call that copies
+ * its rows - so they are current for rows [0, len) whenever a call has returned (in stream order).
+ * ipot_enable_blocks may be called at any time (rows that are in the pot are taken in at once); calling it again with another block_rows
+ * starts anew, with the same one it does nothing.  The first call and such a change synchronise the stream and allocate
+ * 2 * ceil(pot_size / block_rows) rows per unit.  ipot_enable_rope has to come before it (IPOT_E_STATE there otherwise).  block_rows: 16, 32, 64 or 128.
+ * Errors: INVALID, NOMEM, CUDA.
+ */
+int ipot_enable_blocks(ipot_t *pot, int block_rows);
+
+/* Borrowed device pointers to those values, each [layers][batch][Hkv][ceil(pot_size / block_rows)][d] in the pot's dtype, and the number
+ * of blocks that hold rows; what lies behind these is undefined.  Valid until ipot_destroy() or ipot_enable_blocks() with another
+ * block_rows.  Any of lo, hi, n_blocks may be NULL.  STATE unless ipot_enable_blocks was called. */
+int ipot_view_blocks(ipot_t *pot, void **lo, void **hi, int *n_blocks);
+
+/*
+ * One new token's attention over n_blocks blocks per unit, for layers layer .. layer + n_layers - 1: the block of the newest
+ * row, and of the others the n_blocks - 1 with the largest
+ *   s_b = sum over the unit's query heads of sum_c max(q_c lo_bc, q_c hi_bc),
+ * which no head's logit sum over a row of the block exceeds (ties: the lower block; evaluated in 64 bits).  The heads of a unit share the selection.
+ *   q, out, lse : as for ipot_decode_attention, with n_layers in place of layers; the softmax is taken over the selected rows
+ *   blocks      : device int32 [n_layers][batch][Hkv][n_blocks], or NULL: the chosen blocks in ascending order, -1 behind the last
+ *                 where the pot has fewer than n_blocks blocks (all are then chosen)
+ * Everything is fp32 where not said otherwise.  All inputs must be finite.  Asynchronous on the pot's stream; the pot is not changed.
+ * Errors: INVALID (NULL, misaligned, layers outside the pot, n_blocks < 1 or > ceil(pot_size / block_rows)), STATE (len < 1, or
+ * ipot_enable_blocks was not called), CUDA.
+ */
+int ipot_decode_attention_blocks(ipot_t *pot, int layer, int n_layers, const void *q, int n_blocks, float *out, float *lse,
+                                 int32_t *blocks);
+
+/*
  * Borrowed device pointers to the pot ([layers][batch][Hkv][pot_size][d]) and
  * the current fill.  Rows >= len are undefined.  The pointers stay valid until
  * ipot_destroy(); their contents are final once the stream's queued work ran.

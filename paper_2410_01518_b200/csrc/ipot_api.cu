@@ -72,6 +72,9 @@ struct ipot {
                          // calls), then [tokens][segments] float2
     size_t nov_capacity;  // float2 entries behind the counters
     float *stage_aux;
+    // ipot_enable_blocks: bounds of the keys of every block of slots, one allocation; 0 rows: off
+    void *blk_lo, *blk_hi;
+    int blk_rows, blk_count;   // slots of a block, blocks of a unit
     // results of the last cycle
     int last_len_before;
     const float *last_scores;
@@ -127,7 +130,7 @@ int check_config(const ipot_config_t &c)
 
 void free_all(ipot *p)
 {
-    cudaFree(p->arena); cudaFree(p->Krot); cudaFree(p->nov_scratch);
+    cudaFree(p->arena); cudaFree(p->Krot); cudaFree(p->nov_scratch); cudaFree(p->blk_lo);
     if (p->ev_fork) cudaEventDestroy(p->ev_fork);
     if (p->ev_join) cudaEventDestroy(p->ev_join);
     if (p->ev_zero) cudaEventDestroy(p->ev_zero);
@@ -169,6 +172,16 @@ cudaError_t launch_append(ipot *p, dim3 grid, const uint4 *srcK, const uint4 *sr
     return cudaGetLastError();
 }
 
+// Rows [first_row, len) have been written: the bounds of their blocks follow.
+int update_blocks(ipot *p, int first_row, int len)
+{
+    if (!p->blk_rows || first_row >= len) return IPOT_OK;
+    IPOT_CUDA(launch_block_bounds(score_keys(p), p->blk_lo, p->blk_hi, first_row, len, p->blk_rows, p->cfg.d, p->units, p->cfg.pot_size, p->blk_count,
+                                  p->cfg.dtype == IPOT_F32, p->stream));
+    p->launches += 1;
+    return IPOT_OK;
+}
+
 // Copies the rows of a deferred append that are still in the caller's buffers into the pot (keys, values or both).
 int materialise(ipot *p, bool keys, bool values)
 {
@@ -188,7 +201,7 @@ int materialise(ipot *p, bool keys, bool values)
     IPOT_CUDA(cudaGetLastError());
     if (k) p->pend_K = nullptr;
     if (v) p->pend_V = nullptr;
-    return IPOT_OK;
+    return k && !p->rope ? update_blocks(p, p->pend_first, p->pend_first + p->pend_n) : IPOT_OK;
 }
 
 PendingRows pending_rows(const ipot *p)
@@ -504,7 +517,7 @@ int run_cycle(ipot *p, const void *Q, const void *Kc, int cap_rows, const float 
         p->ev_used += 1;
     }
     p->len = keep;
-    return IPOT_OK;
+    return update_blocks(p, 0, keep);
 }
 
 }  // namespace
@@ -895,7 +908,7 @@ int ipot_append_chunk(ipot_t *p, const void *K, const void *V, int n)
             IPOT_CUDA(cudaGetLastError());
         }
         p->len += n;
-        return IPOT_OK;
+        return p->rope ? update_blocks(p, p->len - n, p->len) : IPOT_OK;   // (else the keys are not in the pot yet)
     }
     if (!p->rope) {
         dim3 grid(pieces, p->units, 2);
@@ -907,7 +920,7 @@ int ipot_append_chunk(ipot_t *p, const void *K, const void *V, int n)
     p->launches += 1;
     IPOT_CUDA(cudaGetLastError());
     p->len += n;
-    return IPOT_OK;
+    return update_blocks(p, p->len - n, p->len);
 }
 
 int ipot_append_chunk_host(ipot_t *p, const void *K, const void *V, int n)
@@ -926,7 +939,7 @@ int ipot_append_chunk_host(ipot_t *p, const void *K, const void *V, int n)
         IPOT_CUDA(cudaGetLastError());
     }
     p->len += n;
-    return IPOT_OK;
+    return update_blocks(p, p->len - n, p->len);
 }
 
 int ipot_score_and_compress(ipot_t *p, const void *Q, int cap_rows, const float *aux)
@@ -1059,7 +1072,7 @@ int ipot_enable_rope(ipot_t *p, const void *cos_table, const void *sin_table, in
     if (!p || !cos_table || !sin_table || !aligned16(cos_table) || !aligned16(sin_table)) return IPOT_E_INVALID;
     if (pairing != IPOT_ROPE_HALF && pairing != IPOT_ROPE_INTERLEAVED) return IPOT_E_INVALID;
     if (p->row_bytes % 32) return IPOT_E_INVALID;  // a row must split into two halves of whole 16-byte vectors
-    if (p->len != 0) return IPOT_E_STATE;
+    if (p->len != 0 || p->blk_rows) return IPOT_E_STATE;   // (bounds are those of the keys that are read)
     if (!p->Krot) {
         IPOT_CUDA(cudaStreamSynchronize(p->stream));
         if (cudaMalloc(&p->Krot, (size_t)p->units * p->cfg.pot_size * p->row_bytes) != cudaSuccess) {
@@ -1146,6 +1159,68 @@ int ipot_chunk_attention(ipot_t *p, int layer, int n_layers, int n, const int32_
     c.layers = n_layers; c.streams = p->cfg.batch; c.Hkv = p->cfg.Hkv; c.G = p->G; c.d = p->cfg.d; c.n = n;
     c.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)p->cfg.d));
     IPOT_CUDA(launch_chunk_attention(c, p->cfg.dtype == IPOT_F32, p->stream));
+    p->launches += 1;
+    return IPOT_OK;
+}
+
+int ipot_enable_blocks(ipot_t *p, int block_rows)
+{
+    if (!p || (block_rows != 16 && block_rows != 32 && block_rows != 64 && block_rows != 128)) return IPOT_E_INVALID;
+    if (block_rows == p->blk_rows) return IPOT_OK;
+    DeviceGuard device(p->device);
+    if (!device.ok) return IPOT_E_CUDA;
+    int rc = materialise(p, true, true);
+    if (rc != IPOT_OK) return rc;
+    IPOT_CUDA(cudaStreamSynchronize(p->stream));
+    const int count = (p->cfg.pot_size + block_rows - 1) / block_rows;
+    const size_t bytes = ((size_t)p->units * count * p->row_bytes + 255) / 256 * 256;
+    void *mem = nullptr;
+    if (cudaMalloc(&mem, 2 * bytes) != cudaSuccess) {
+        cudaGetLastError();
+        return IPOT_E_NOMEM;
+    }
+    cudaFree(p->blk_lo);
+    p->blk_lo = mem;
+    p->blk_hi = (char *)mem + bytes;
+    p->blk_rows = block_rows;
+    p->blk_count = count;
+    return update_blocks(p, 0, p->len);
+}
+
+int ipot_view_blocks(ipot_t *p, void **lo, void **hi, int *n_blocks)
+{
+    if (!p) return IPOT_E_INVALID;
+    if (!p->blk_rows) return IPOT_E_STATE;
+    DeviceGuard device(p->device);
+    if (!device.ok) return IPOT_E_CUDA;
+    int rc = materialise(p, true, true);
+    if (rc != IPOT_OK) return rc;
+    if (lo) *lo = p->blk_lo;
+    if (hi) *hi = p->blk_hi;
+    if (n_blocks) *n_blocks = (p->len + p->blk_rows - 1) / p->blk_rows;
+    return IPOT_OK;
+}
+
+int ipot_decode_attention_blocks(ipot_t *p, int layer, int n_layers, const void *q, int n_blocks, float *out, float *lse, int32_t *blocks)
+{
+    if (!p || !q || !out || !aligned16(q) || ((reinterpret_cast<uintptr_t>(out) | reinterpret_cast<uintptr_t>(lse) | reinterpret_cast<uintptr_t>(blocks)) & 3u))
+        return IPOT_E_INVALID;
+    if (layer < 0 || n_layers < 1 || layer > p->cfg.layers - n_layers || n_blocks < 1) return IPOT_E_INVALID;
+    if (!p->blk_rows) return IPOT_E_STATE;
+    if (n_blocks > p->blk_count) return IPOT_E_INVALID;
+    if (p->len < 1) return IPOT_E_STATE;
+    DeviceGuard device(p->device);
+    if (!device.ok) return IPOT_E_CUDA;
+    int rc = materialise(p, true, true);
+    if (rc != IPOT_OK) return rc;
+    BlocksParams b;
+    b.q = q; b.K = score_keys(p); b.V = p->V; b.lo = p->blk_lo; b.hi = p->blk_hi;
+    b.out = out; b.lse = lse; b.list = blocks;
+    b.unit0 = layer * p->cfg.batch * p->cfg.Hkv;
+    b.unit_rows = p->cfg.pot_size; b.unit_blocks = p->blk_count; b.len = p->len; b.rows = p->blk_rows; b.blocks = n_blocks;
+    b.layers = n_layers; b.streams = p->cfg.batch; b.Hkv = p->cfg.Hkv; b.G = p->G; b.d = p->cfg.d;
+    b.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)p->cfg.d));
+    IPOT_CUDA(launch_decode_blocks(b, p->cfg.dtype == IPOT_F32, p->sm_count, p->stream));
     p->launches += 1;
     return IPOT_OK;
 }

@@ -1,6 +1,7 @@
 // Kernels of the operators around the pot and their launchers: a second compilation unit beside ipot_api.cu.
 #include "ops.h"
 
+#include "k_blocks.cuh"
 #include "k_chunk_fma.cuh"
 #include "k_rotary.cuh"
 
@@ -27,6 +28,23 @@ cudaError_t launch_rope_rows(const RopeRowsParams &p, bool f32, bool table_f32, 
 cudaError_t launch_chunk_attention(const ChunkParams &p, bool f32, cudaStream_t stream)
 {
     return f32 ? launch_chunk_fma<float>(p, stream) : launch_chunk_fma<__nv_bfloat16>(p, stream);
+}
+
+cudaError_t launch_block_bounds(const void *K, void *lo, void *hi, int first_row, int len, int rows, int d, int units, size_t unit_rows, int unit_blocks, bool f32,
+                                cudaStream_t stream)
+{
+    return f32 ? launch_block_bounds_t<float>(K, lo, hi, first_row, len, rows, d, units, unit_rows, unit_blocks, stream)
+               : launch_block_bounds_t<__nv_bfloat16>(K, lo, hi, first_row, len, rows, d, units, unit_rows, unit_blocks, stream);
+}
+
+cudaError_t launch_decode_blocks(const BlocksParams &p, bool f32, int sm_count, cudaStream_t stream)
+{
+    // blocks of a cluster: enough for every SM to have one or two, and none without a few dozen rows
+    const long long units = (long long)p.layers * p.streams * p.Hkv * ((p.G + kBlkHeads - 1) / kBlkHeads);
+    const int rows = p.blocks < (p.len + p.rows - 1) / p.rows ? p.blocks * p.rows : p.len;
+    int cluster = 1;
+    while (cluster < 8 && units * cluster * 2 <= 2LL * sm_count && rows / cluster >= 64) cluster *= 2;
+    return f32 ? launch_blocks<float>(p, cluster, stream) : launch_blocks<__nv_bfloat16>(p, cluster, stream);
 }
 
 }  // namespace ipotk

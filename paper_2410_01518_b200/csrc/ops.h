@@ -51,4 +51,20 @@ struct ChunkParams {
 };
 cudaError_t launch_chunk_attention(const ChunkParams &p, bool f32, cudaStream_t stream);
 
+// ------------------------------------------------------------------ generation over selected blocks (k_blocks.cuh)
+struct BlocksParams {
+    const void *q;                 // [layers][streams][Hkv * G][d]
+    const void *K, *V;             // [units][unit_rows][d], from the pot's first unit on
+    const void *lo, *hi;           // [units][unit_blocks][d]
+    float *out, *lse;              // of the layers asked for
+    int32_t *list;                 // [layers][streams][Hkv][blocks], or NULL
+    int unit0, unit_rows, unit_blocks, len, rows, blocks;
+    int layers, streams, Hkv, G, d;
+    float scale_log2e;
+};
+cudaError_t launch_decode_blocks(const BlocksParams &p, bool f32, int sm_count, cudaStream_t stream);
+// bounds of the blocks that hold rows [first_row, len) of every unit
+cudaError_t launch_block_bounds(const void *K, void *lo, void *hi, int first_row, int len, int rows, int d, int units, size_t unit_rows, int unit_blocks, bool f32,
+                                cudaStream_t stream);
+
 }  // namespace ipotk

@@ -34,7 +34,7 @@ SYMBOLS = [
     "ipot_score_and_compress_cap", "ipot_score_only_cap", "ipot_score_and_compress_cap_host",
     "ipot_nuc_scores", "ipot_enable_rope", "ipot_view_rope",
     "ipot_decode_attention", "ipot_set_tuning", "ipot_rope_tables", "ipot_rope_rows",
-    "ipot_chunk_attention",
+    "ipot_chunk_attention", "ipot_enable_blocks", "ipot_view_blocks", "ipot_decode_attention_blocks",
 ]
 
 
@@ -105,6 +105,9 @@ def lib() -> C.CDLL:
         L.ipot_rope_tables.argtypes = [C.POINTER(ipot_rope_spec_t), C.c_longlong, ip, ip, vp, vp, vp]
         L.ipot_rope_rows.argtypes = [vp, C.POINTER(ipot_rope_t), ip, ip, vp, ip, vp, st, vp, st, vp, st, vp, st]
         L.ipot_chunk_attention.argtypes = [vp, ip, ip, ip, vp, vp, st, vp, st, vp, st, vp, st, vp]
+        L.ipot_enable_blocks.argtypes = [vp, ip]
+        L.ipot_view_blocks.argtypes = [vp, C.POINTER(vp), C.POINTER(vp), C.POINTER(ip)]
+        L.ipot_decode_attention_blocks.argtypes = [vp, ip, ip, vp, ip, vp, vp, vp]
         L.ipot_view.argtypes = [vp, C.POINTER(vp), C.POINTER(vp), C.POINTER(ip)]
         L.ipot_last_indices.argtypes = [vp, C.POINTER(vp)]
         L.ipot_last_scores.argtypes = [vp, C.POINTER(vp), C.POINTER(ip)]
@@ -262,6 +265,22 @@ def ipot_chunk_attention(h, layer, n_layers, n_tokens, q, k, v, out, lse=None, t
                          out_strides=None) -> None:
     _check(lib().ipot_chunk_attention(h, layer, n_layers, n_tokens, _ptr(tokens), _ptr(q), _strides(q_strides), _ptr(k), _strides(k_strides),
                                       _ptr(v), _strides(v_strides), _ptr(out), _strides(out_strides), _ptr(lse)), "ipot_chunk_attention")
+
+
+def ipot_enable_blocks(h, block_rows) -> None:
+    _check(lib().ipot_enable_blocks(h, block_rows), "ipot_enable_blocks")
+
+
+def ipot_view_blocks(h):
+    """-> (device address of the lower bounds, of the upper bounds, blocks that hold rows)."""
+    lo, hi, n = C.c_void_p(), C.c_void_p(), C.c_int()
+    _check(lib().ipot_view_blocks(h, C.byref(lo), C.byref(hi), C.byref(n)), "ipot_view_blocks")
+    return lo.value, hi.value, n.value
+
+
+def ipot_decode_attention_blocks(h, layer, n_layers, q, n_blocks, out, lse=None, blocks=None) -> None:
+    _check(lib().ipot_decode_attention_blocks(h, layer, n_layers, _ptr(q), n_blocks, _ptr(out), _ptr(lse), _ptr(blocks)),
+           "ipot_decode_attention_blocks")
 
 
 def ipot_view(h):
