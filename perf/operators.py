@@ -349,7 +349,7 @@ def _own_state(c, s):
     s.ipot = ipot
     if c["kind"] == "tables":
         return
-    n = c.get("len", c["n"])
+    n = c["len"] if "len" in c else c["n"]
 
     class Pot:
         def __init__(self):
