@@ -1158,7 +1158,9 @@ int ipot_chunk_attention(ipot_t *p, int layer, int n_layers, int n, const int32_
     c.unit_rows = p->cfg.pot_size; c.len = p->len;
     c.layers = n_layers; c.streams = p->cfg.batch; c.Hkv = p->cfg.Hkv; c.G = p->G; c.d = p->cfg.d; c.n = n;
     c.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)p->cfg.d));
-    IPOT_CUDA(launch_chunk_attention(c, p->cfg.dtype == IPOT_F32, p->stream));
+    c.status = p->status;
+    const ChunkTcHost host{(void *)p->tc.encode, p->sm_count, p->units, p->ts.withhold_rank, p->ts.wait_ns};
+    IPOT_CUDA(launch_chunk_attention(c, p->cfg.dtype == IPOT_F32, host, p->stream));
     p->launches += 1;
     return IPOT_OK;
 }

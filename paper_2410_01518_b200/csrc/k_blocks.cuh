@@ -88,6 +88,7 @@ __device__ __forceinline__ uint32_t cluster_size()
 }
 __device__ __forceinline__ void cluster_sync()
 {
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // The address of `p`, a pointer into this block's shared memory, in block `rank` of the cluster.

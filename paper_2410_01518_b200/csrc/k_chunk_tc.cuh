@@ -1,0 +1,554 @@
+// Attention of a chunk of new tokens over the pot and, causally, over itself, on the 5th-generation tensor cores (bf16).
+//
+// The query heads of a KV head share its keys: a unit's rows are folded token by token, row t * G + g, and a query tile is the
+// rows of floor(128 / G) tokens (TMA fetches it as a box of G heads x tokens, whatever the strides).  Keys come in tiles of KT,
+// first the pot's, then the chunk's.  Per tile and stream
+//   S = Q K^T   128 x KT fp32 in tensor memory (both operands in shared memory, K-major, 128-byte swizzle)
+//   softmax     a thread owns a row: p = 2^(s c - m) against a reference m that is only moved when the row's maximum passes it by
+//               2^8 (then the row's sums and output are scaled down: rare), l += p in fp32, and p as bf16 over S in tensor memory
+//   O += P V    P from tensor memory, V as it lies (channels contiguous: the N-major operand layout), 128 x D fp32 in tensor memory
+// A block runs two streams so that the tensor core works on one while the other's softmax runs: two query tiles that share the
+// key tiles (kSplit = false), or one query tile whose key tiles take turns (kSplit, for calls of few rows; merged at the
+// end).  More than 128 channels: one stream, tensor memory holds one output.  Calls with fewer query tiles than
+// SMs spread a tile's keys over a cluster whose blocks merge their results through distributed shared memory: nothing is
+// exchanged through global memory, and the result does not depend on timing.
+//
+// Warps: 0 loads (TMA), 1 issues the products, 2-5 / 6-9 softmax of the two streams.  All waits are bounded (wait_ns): one that runs out
+// raises the block's give-up flag and IPOT_E_TIMEOUT; from then on nothing more is put in flight, and what is in flight is
+// waited for before tensor memory is released.
+#pragma once
+#include "k_blocks.cuh"   // cluster_*
+#include "k_chunk_fma.cuh"
+#include "ops.h"
+#include "ptx.cuh"
+
+namespace ipotk {
+
+constexpr int kCtRows = 128;
+constexpr float kChunkSlack = 8.f;   // binary orders by which a row's maximum may pass its reference
+
+template <int D, bool kSplit> struct ChunkTc {
+    static constexpr int kStreams = D > 128 ? 1 : 2;
+    static constexpr int kQTiles = kSplit ? 1 : 2;
+    static constexpr int kKeys = D > 128 ? 64 : 128;
+    static constexpr int kHalves = D / 64;                                   // blocks of 64 channels
+    static constexpr uint32_t kKeyBlk = kKeys * 128, kStageBytes = kHalves * kKeyBlk;
+    static constexpr uint32_t kQBlk = kCtRows * 128, kQBytes = kHalves * kQBlk;
+    static constexpr int kStages = D == 64 ? 8 : D == 128 && kSplit ? 6 : 5;
+    static constexpr int kPitch = D + 4;                                     // of a row of a partial result
+    static constexpr uint32_t kOffStage = 0, kOffQ = kStages * kStageBytes, kOffStat = kOffQ + kQTiles * kQBytes;   // [2][128] float2
+    static constexpr uint32_t kOffBar = kOffStat + kStreams * kCtRows * 8, kOffFlag = kOffBar + 8 * 32, kSmemBytes = kOffFlag + 16;
+    static constexpr uint32_t kOutCol = 256;                                 // tensor memory: S of stream i at 128 i, O at 256 + D i
+    static constexpr int kThreads = 64 + 128 * kStreams;
+    static_assert(kStreams * kCtRows * kPitch * 4 <= kStages * kStageBytes, "partial results take the stages' place");
+    static_assert(kSmemBytes <= 232448, "shared memory of a block");
+};
+enum { kCbQ = 0, kCbFull = 1, kCbEmpty = 9, kCbS = 17, kCbP = 19, kCbO = 21, kCbDrain = 23 };
+
+// D[M x N] += A B with A in tensor memory (a row per lane, two bf16 per column).
+__device__ __forceinline__ void tc_mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+// An N-major operand with 128-byte swizzle: blocks of 64 columns `blk` bytes apart, 8 rows of K 1024 bytes apart.
+__device__ __forceinline__ uint64_t smem_desc_sw128_nmajor(uint32_t addr, uint32_t blk)
+{
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)(blk >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+}
+__device__ __forceinline__ void tma_load_5d(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, int c3, int c4, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+        ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(c4), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&v)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+        ::"r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]),
+          "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]),
+          "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]),
+          "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]),
+          "r"(taddr) : "memory");
+}
+
+// A wait of at most wait_ns from its start.  flag: the block's give-up flag; with heed_flag off it is a role's wait for what it has itself put in flight.
+__device__ __forceinline__ bool chunk_wait(uint32_t bar, uint32_t parity, volatile int *flag, const ChunkTcParams &p, bool heed_flag = true)
+{
+    unsigned long long t0 = 0;
+    for (uint32_t i = 0;; ++i) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if ((i & 1023u) == 1023u) {
+            if (heed_flag && *flag) return false;
+            const unsigned long long now = global_timer_ns();
+            if (!t0) t0 = now;
+            if (now - t0 > p.wait_ns) {
+                *flag = 1;
+                set_status(p.status, kStatusTimeout);
+                return false;
+            }
+        }
+    }
+}
+
+// grid: cluster x (row tiles or pairs of them, the longest first) x units.
+template <int D, bool kSplit>
+__global__ void __launch_bounds__(ChunkTc<D, kSplit>::kThreads, 1)
+chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant__ CUtensorMap mapK, const __grid_constant__ CUtensorMap mapV,
+                const __grid_constant__ CUtensorMap mapKnew, const __grid_constant__ CUtensorMap mapVnew, const __grid_constant__ ChunkTcParams p)
+{
+    using L = ChunkTc<D, kSplit>;
+    constexpr int S = L::kStreams, KT = L::kKeys;
+    extern __shared__ __align__(1024) uint8_t ct_raw[];
+    const uint32_t base = smem_u32(ct_raw);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank(), ranks = cluster_size();
+    auto bar = [&](int i) { return base + L::kOffBar + 8u * (uint32_t)i; };
+    volatile int *flag = reinterpret_cast<volatile int *>(ct_raw + L::kOffFlag);
+    uint32_t *tmem_slot = reinterpret_cast<uint32_t *>(ct_raw + L::kOffFlag + 8);
+    if (base & 1023u) {   // the swizzled tiles need this alignment
+        if (threadIdx.x == 0) set_status(p.c.status, kStatusBounds);
+        return;
+    }
+    // ---- which rows and keys
+    const int units = p.c.layers * p.c.streams * p.c.Hkv, item = blockIdx.x / ranks, unit = item % units;
+    const int tile0 = (p.items_per_unit - 1 - item / units) * L::kQTiles;   // of kCtRows rows: p.tile_tokens tokens
+    const int hkv = unit % p.c.Hkv, b = unit / p.c.Hkv % p.c.streams, l = unit / p.c.Hkv / p.c.streams;
+    if (threadIdx.x == 0) {
+        *flag = 0;
+        for (int i = 0; i < kCbDrain + 1; ++i) mbar_init(bar(i), i >= kCbP && i < kCbO ? 4 : 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    pdl_wait();
+    pdl_release();
+    const int n = chunk_tokens(p.c, b), G = p.c.G, t0 = tile0 * p.tile_tokens;
+    // tokens of the query tiles, and the key tiles they need: the pot's, then the chunk's up to the last token
+    const int tokens[2] = {min(p.tile_tokens, n - t0), kSplit ? 0 : min(p.tile_tokens, n - t0 - p.tile_tokens)};
+    const int seen = min(n, t0 + L::kQTiles * p.tile_tokens);   // chunk tokens that some row sees
+    const int pot_tiles = (p.c.len + KT - 1) / KT, all_tiles = t0 < n ? pot_tiles + (seen + KT - 1) / KT : 0;
+    const int first = (int)((long long)all_tiles * rank / ranks), tiles = (int)((long long)all_tiles * (rank + 1) / ranks) - first;
+    const int pot_unit = p.c.unit0 + unit;
+
+    if (warp == 0) {
+        // ---------------------------------------------------------------- loads
+        if (lane == 0 && tiles > 0) {
+            mbar_expect_tx(bar(kCbQ), L::kQTiles * L::kHalves * (uint32_t)(p.tile_tokens * G * 128));
+            for (int i = 0; i < L::kQTiles; ++i)
+                for (int h = 0; h < L::kHalves; ++h)
+                    tma_load_5d(base + L::kOffQ + i * L::kQBytes + h * L::kQBlk, &mapQ, 64 * h, hkv * G, t0 + i * p.tile_tokens, b, l, bar(kCbQ));
+            uint32_t k = 0;   // loads so far
+            bool ok = true;
+            auto load = [&](int t, bool values) {
+                const uint32_t slot = k % L::kStages, fill = k / L::kStages, dst = base + L::kOffStage + slot * L::kStageBytes;
+                ok = ok && chunk_wait(bar(kCbEmpty + slot), (fill & 1) ^ 1, flag, p);
+                if (!ok) return;
+                mbar_expect_tx(bar(kCbFull + slot), L::kStageBytes);
+                const int tile = first + t;
+                if (tile < pot_tiles) {
+                    for (int h = 0; h < L::kHalves; ++h) tma_load_3d(dst + h * L::kKeyBlk, values ? &mapV : &mapK, 64 * h, tile * KT, pot_unit, bar(kCbFull + slot));
+                } else {
+                    for (int h = 0; h < L::kHalves; ++h)
+                        tma_load_5d(dst + h * L::kKeyBlk, values ? &mapVnew : &mapKnew, 64 * h, (tile - pot_tiles) * KT, hkv, b, l, bar(kCbFull + slot));
+                }
+                ++k;
+            };
+            constexpr int ahead = kSplit ? S : 1;   // tiles whose logits are under way before the first output product
+            for (int t = 0; t < min(ahead, tiles); ++t) load(t, false);
+            for (int t = 0; t < tiles && ok; ++t) {
+                load(t, true);
+                if (t + ahead < tiles) load(t + ahead, false);
+            }
+            // what was issued lands in this block's shared memory: the last load of every slot completes before the block ends
+            chunk_wait(bar(kCbQ), 0, flag, p, false);
+            for (uint32_t j = k > (uint32_t)L::kStages ? k - L::kStages : 0; j < k; ++j) chunk_wait(bar(kCbFull + j % L::kStages), (j / L::kStages) & 1, flag, p, false);
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // ---------------------------------------------------------------- products
+        const bool leader = elect_one();
+        const uint32_t idesc_s = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(KT >> 3) << 17) | ((128u >> 4) << 24);
+        const uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)((p.c.d + 15) / 16 * 2) << 17) | ((128u >> 4) << 24);
+        const int ksteps = (p.c.d + 15) / 16;
+        uint32_t k = 0;   // stages used so far
+        bool ok = tiles > 0, any = false;
+        auto wait = [&](int which, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, chunk_wait(bar(which), parity, flag, p)); };
+        auto wait_stage = [&](uint32_t at) { wait(kCbFull + at % L::kStages, (at / L::kStages) & 1); };
+        auto logits = [&](int i, uint32_t at) {   // S of stream i from stage `at`
+            any = true;
+            const uint64_t a = smem_desc_sw128(base + L::kOffQ + (kSplit ? 0 : i) * L::kQBytes), bd = smem_desc_sw128(base + L::kOffStage + at % L::kStages * L::kStageBytes);
+            if (leader) {
+                for (int c = 0; c < ksteps; ++c)
+                    tc_mma_bf16(tmem + 128 * i, a + (c >> 2) * (L::kQBlk >> 4) + 2 * (c & 3), bd + (c >> 2) * (L::kKeyBlk >> 4) + 2 * (c & 3), idesc_s, c > 0);
+                tc_commit(bar(kCbS + i));
+            }
+            __syncwarp();
+        };
+        auto output = [&](int i, uint32_t at, bool more) {   // O of stream i += P V
+            any = true;
+            const uint64_t bd = smem_desc_sw128_nmajor(base + L::kOffStage + at % L::kStages * L::kStageBytes, L::kKeyBlk);
+            if (leader) {
+#pragma unroll
+                for (int c = 0; c < KT / 16; ++c)
+                    tc_mma_bf16_ts(tmem + L::kOutCol + D * i, tmem + 128 * i + 8 * c, bd + c * (16 * 128 >> 4), idesc_o, more || c > 0);
+            }
+            __syncwarp();
+        };
+        auto release = [&](uint32_t at) {
+            if (leader) tc_commit(bar(kCbEmpty + at % L::kStages));
+            __syncwarp();
+        };
+        // Values behind a stream's last token count for nothing but must be finite: 0 times what lies there is not 0 otherwise.
+        auto clear_padding = [&](int t, uint32_t at) {
+            const int tile = first + t, from = n - (tile - pot_tiles) * KT;
+            if (tile < pot_tiles || from >= KT || n == p.c.n) return;
+            uint8_t *v = ct_raw + L::kOffStage + at % L::kStages * L::kStageBytes;
+            for (int h = 0; h < L::kHalves; ++h)
+                for (int e = from * 8 + lane; e < KT * 8; e += 32) *reinterpret_cast<uint4 *>(v + h * L::kKeyBlk + e * 16) = make_uint4(0, 0, 0, 0);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+        };
+        wait(kCbQ, 0);
+        if (kSplit) {
+            for (int t = 0; t < min(S, tiles) && ok; ++t, ++k) {
+                wait_stage(k);
+                if (!ok) break;
+                tc_fence_after();
+                logits(t, k);
+                release(k);
+            }
+            for (int t = 0; t < tiles && ok; ++t) {
+                const int i = t % S;
+                wait_stage(k);
+                wait(kCbP + i, (t / S) & 1);
+                if (!ok) break;
+                tc_fence_after();
+                clear_padding(t, k);
+                output(i, k, t >= S);
+                release(k++);
+                if (t + S < tiles) {
+                    wait_stage(k);
+                    if (!ok) break;
+                    logits(i, k);
+                    release(k++);
+                } else if (leader) {
+                    tc_commit(bar(kCbO + i));
+                }
+                __syncwarp();
+            }
+        } else {
+            const int live = tokens[1] > 0 ? 2 : 1;
+            wait_stage(0);
+            tc_fence_after();
+            for (int i = 0; i < live && ok; ++i) logits(i, 0);
+            if (ok) release(0);
+            k = 1;
+            for (int t = 0; t < tiles && ok; ++t) {
+                const uint32_t kv = k, kk = k + 1;
+                const bool last = t + 1 == tiles;
+                wait_stage(kv);
+                for (int i = 0; i < live && ok; ++i) {
+                    wait(kCbP + i, t & 1);
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (i == 0) clear_padding(t, kv);
+                    output(i, kv, t > 0);
+                    if (i + 1 == live) release(kv);
+                    if (!last) {
+                        if (i == 0) wait_stage(kk);
+                        if (!ok) break;
+                        logits(i, kk);
+                        if (i + 1 == live) release(kk);
+                    } else if (leader) {
+                        tc_commit(bar(kCbO + i));
+                    }
+                    __syncwarp();
+                }
+                k += last ? 1 : 2;
+            }
+        }
+        if (any) {   // every product has finished before tensor memory is released
+            if (leader) tc_commit(bar(kCbDrain));
+            chunk_wait(bar(kCbDrain), 0, flag, p, false);
+        }
+        __syncwarp();
+    } else {
+        // ---------------------------------------------------------------- softmax
+        const int i = S == 1 ? 0 : (warp - 2) >> 2, q = warp & 3, row = q * 32 + lane;   // (a warp may touch the TMEM lanes of its quarter)
+        const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16), ts = lanes + 128 * i, to = lanes + L::kOutCol + D * i;
+        const int qt = kSplit ? 0 : i, ti = row / G, t = t0 + qt * p.tile_tokens + ti, g = row - ti * G;
+        const bool valid = ti < tokens[qt], works = __any_sync(0xffffffffu, valid);
+        const int mine = tiles <= 0 || tokens[qt] <= 0 ? 0 : kSplit ? (tiles - i + S - 1) / S : tiles;
+        const float c = p.c.scale_log2e;
+        float m = -INFINITY, sum = 0.f;
+        for (int j = 0; j < mine; ++j) {
+            const int tile = first + (kSplit ? j * S + i : j);
+            // columns that this row sees
+            const int cols = tile < pot_tiles ? min(KT, p.c.len - tile * KT) : min(KT, t + 1 - (tile - pot_tiles) * KT);
+            const bool masked = __any_sync(0xffffffffu, valid && cols < KT);
+            chunk_wait(bar(kCbS + i), j & 1, flag, p);
+            __syncwarp();
+            tc_fence_after();
+            if (works) {
+                uint32_t v[KT / 32][32];
+#pragma unroll
+                for (int a = 0; a < KT / 32; ++a) tmem_ld32(ts + 32 * a, v[a]);
+#pragma unroll
+                for (int a = 0; a < KT / 32; ++a) tmem_wait_ld(v[a]);
+                if (masked) {
+#pragma unroll
+                    for (int a = 0; a < KT / 32; ++a)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (32 * a + e >= cols) v[a][e] = __float_as_uint(-INFINITY);
+                }
+                float mx[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) mx[e] = max3(__uint_as_float(v[0][e]), __uint_as_float(v[0][e + 4]), __uint_as_float(v[0][e + 8]));
+#pragma unroll
+                for (int a = 0; a < KT / 32; ++a)
+#pragma unroll
+                    for (int e = a ? 0 : 12; e + 8 <= 32; e += 8)
+#pragma unroll
+                        for (int f = 0; f < 4; ++f) mx[f] = max3(mx[f], __uint_as_float(v[a][e + f]), __uint_as_float(v[a][e + f + 4]));
+#pragma unroll
+                for (int f = 0; f < 4; ++f) mx[f] = fmaxf(mx[f], __uint_as_float(v[0][28 + f]));
+                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
+                const bool moves = valid && top > m + kChunkSlack;
+                if (__any_sync(0xffffffffu, moves)) {
+                    const float to_m = moves ? top : m, f = moves ? chunk_ex2(m - to_m) : 1.f;   // (m = -inf: 0)
+                    sum *= f;
+                    m = to_m;
+                    if (j > 0) {
+                        // the product that last added to O has finished: it was issued before the one that made this tile's logits
+#pragma unroll 1
+                        for (int a = 0; a < D / 32; ++a) {
+                            uint32_t o[32];
+                            tmem_ld32(to + 32 * a, o);
+                            tmem_wait_ld(o);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            tmem_st32(to + 32 * a, o);
+                        }
+                    }
+                }
+                const float ref = m == -INFINITY ? 0.f : m;
+                const float2 c2 = make_float2(c, c), r2 = make_float2(-ref, -ref);
+                float2 s2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+                for (int a = 0; a < KT / 32; ++a)
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        const float2 x = __ffma2_rn(make_float2(__uint_as_float(v[a][e]), __uint_as_float(v[a][e + 1])), c2, r2);
+                        const float2 w = make_float2(chunk_ex2(x.x), chunk_ex2(x.y));
+                        s2[(e >> 1) & 1] = __fadd2_rn(s2[(e >> 1) & 1], w);
+                        const __nv_bfloat162 h = __floats2bfloat162_rn(w.x, w.y);
+                        v[a >> 1][(a & 1) * 16 + (e >> 1)] = *reinterpret_cast<const uint32_t *>(&h);   // (two columns become one: what is overwritten has been used)
+                    }
+                const float2 s1 = __fadd2_rn(s2[0], s2[1]);
+                sum += s1.x + s1.y;
+#pragma unroll
+                for (int a = 0; a < KT / 64; ++a) tmem_st32(ts + 32 * a, v[a]);
+                tmem_wait_st();
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0 && p.withhold != i) mbar_arrive(bar(kCbP + i));
+        }
+        if (mine > 0) {
+            chunk_wait(bar(kCbO + i), 0, flag, p);
+            __syncwarp();
+            tc_fence_after();
+        }
+        if (!p.merge) {
+            if (works && mine > 0) {   // (mine > 0 is uniform over the stream)
+                const float inv = 1.f / sum;
+                __nv_bfloat16 *o = (__nv_bfloat16 *)p.c.out + l * p.c.os.layer + b * p.c.os.stream + (long long)(hkv * G + g) * p.c.os.head + (long long)t * p.c.os.token;
+#pragma unroll 1
+                for (int a = 0; a < D / 32; ++a) {
+                    uint32_t x[32];
+                    tmem_ld32(to + 32 * a, x);
+                    tmem_wait_ld(x);
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int f = 0; f < 4; ++f) {
+                            const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(x[e + 2 * f]) * inv, __uint_as_float(x[e + 2 * f + 1]) * inv);
+                            w[f] = *reinterpret_cast<const uint32_t *>(&h);
+                        }
+                        if (valid && 32 * a + e < p.c.d) *reinterpret_cast<uint4 *>(o + 32 * a + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
+                if (valid && p.c.lse) p.c.lse[(((size_t)l * p.c.streams + b) * p.c.Hkv * G + hkv * G + g) * p.c.n + t] = 0.6931471805599453f * (m + log2f(sum));
+            }
+        } else if (works) {
+            // this stream's result into shared memory (the stages have been read: every product of this stream, and with it every key tile
+            // that it waits for, is done; the other stream's are in the way only after its own wait, hence the barrier below)
+            reinterpret_cast<float2 *>(ct_raw + L::kOffStat)[i * kCtRows + row] = make_float2(m, sum);
+        }
+    }
+    if (p.merge) {
+        tc_fence_before();
+        __syncthreads();   // all products are done: the stages' memory is free
+        tc_fence_after();
+        float *part = reinterpret_cast<float *>(ct_raw + L::kOffStage);
+        float2 *stat = reinterpret_cast<float2 *>(ct_raw + L::kOffStat);
+        if (warp >= 2) {
+            const int i = S == 1 ? 0 : (warp - 2) >> 2, q = warp & 3, row = q * 32 + lane, qt = kSplit ? 0 : i;
+            const bool works = __any_sync(0xffffffffu, row / G < tokens[qt]);
+            const int mine = tiles <= 0 ? 0 : kSplit ? (tiles - i + S - 1) / S : tiles;
+            if (works && mine > 0) {
+                const uint32_t to = tmem + ((uint32_t)(q * 32) << 16) + L::kOutCol + D * i;
+                float4 *dst = reinterpret_cast<float4 *>(part + (size_t)(i * kCtRows + row) * L::kPitch);
+#pragma unroll 1
+                for (int a = 0; a < D / 32; ++a) {
+                    uint32_t x[32];
+                    tmem_ld32(to + 32 * a, x);
+                    tmem_wait_ld(x);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        dst[a * 8 + e] = make_float4(__uint_as_float(x[4 * e]), __uint_as_float(x[4 * e + 1]), __uint_as_float(x[4 * e + 2]), __uint_as_float(x[4 * e + 3]));
+                }
+            } else if (works) {
+                stat[i * kCtRows + row] = make_float2(-INFINITY, 0.f);
+            }
+        }
+        cluster_sync();
+        // a thread has 8 channels of a row; partial results of the cluster's blocks and, where the streams share a query tile, of both streams
+        const int vecs = p.c.d / 8, parts = kSplit ? S : 1;
+        for (int qt = 0; qt < L::kQTiles; ++qt) {
+            const int rows = max(tokens[qt], 0) * G;
+            for (int e = rank * L::kThreads + threadIdx.x; e < rows * vecs; e += ranks * L::kThreads) {
+                const int row = e / vecs, v = e - row * vecs;
+                float ref = -INFINITY, den = 0.f, o[8];
+#pragma unroll
+                for (int f = 0; f < 8; ++f) o[f] = 0.f;
+                for (uint32_t r = 0; r < ranks; ++r)
+                    for (int i = 0; i < parts; ++i) ref = fmaxf(ref, cluster_ld(cluster_addr(&stat[(qt + i) * kCtRows + row].x, r)));
+                for (uint32_t r = 0; r < ranks; ++r)
+                    for (int i = 0; i < parts; ++i) {
+                        const uint32_t st = cluster_addr(&stat[(qt + i) * kCtRows + row], r), src = cluster_addr(part + (size_t)((qt + i) * kCtRows + row) * L::kPitch + 8 * v, r);
+                        const float mr = cluster_ld(st);
+                        if (mr == -INFINITY) continue;   // it has seen no key of this row: what it holds is not a number
+                        const float f = chunk_ex2(mr - ref);
+                        den = fmaf(cluster_ld(st + 4), f, den);
+#pragma unroll
+                        for (int x = 0; x < 8; ++x) o[x] = fmaf(cluster_ld(src + 4 * x), f, o[x]);
+                    }
+                const float inv = 1.f / den;
+                uint32_t w[4];
+#pragma unroll
+                for (int f = 0; f < 4; ++f) {
+                    const __nv_bfloat162 h = __floats2bfloat162_rn(o[2 * f] * inv, o[2 * f + 1] * inv);
+                    w[f] = *reinterpret_cast<const uint32_t *>(&h);
+                }
+                const int ti = row / G, g = row - ti * G, t = t0 + qt * p.tile_tokens + ti;
+                __nv_bfloat16 *out = (__nv_bfloat16 *)p.c.out + l * p.c.os.layer + b * p.c.os.stream + (long long)(hkv * G + g) * p.c.os.head + (long long)t * p.c.os.token;
+                *reinterpret_cast<uint4 *>(out + 8 * v) = make_uint4(w[0], w[1], w[2], w[3]);
+                if (v == 0 && p.c.lse) p.c.lse[(((size_t)l * p.c.streams + b) * p.c.Hkv * G + hkv * G + g) * p.c.n + t] = 0.6931471805599453f * (ref + log2f(den));
+            }
+        }
+        cluster_sync();   // no block ends while others read its results
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+}
+
+// ------------------------------------------------------------------ host side
+// [layer][stream][head][token][d] bf16 as a map of five dimensions, whatever the strides; a box is 64 channels of `heads` heads x `tokens` tokens (heads inside)
+// or, keys, of `tokens` tokens of one head.
+inline bool chunk_map(TcEncodeFn encode, CUtensorMap *map, const void *ptr, const ChunkParams &p, const Strides &s, int heads_all, bool queries, int heads, int tokens)
+{
+    // a stride that no second element ever uses may be anything: one that is always allowed stands in
+    auto bytes = [](long long stride, int extent, long long other) { return (cuuint64_t)(2 * (extent > 1 ? stride : other)); };
+    const cuuint64_t st_h = bytes(s.head, heads_all, p.d), st_t = bytes(s.token, p.n, p.d), st_b = bytes(s.stream, p.streams, p.d), st_l = bytes(s.layer, p.layers, p.d);
+    const cuuint64_t dims[5] = {(cuuint64_t)p.d, (cuuint64_t)(queries ? heads_all : p.n), (cuuint64_t)(queries ? p.n : heads_all), (cuuint64_t)p.streams, (cuuint64_t)p.layers};
+    const cuuint64_t strides[4] = {queries ? st_h : st_t, queries ? st_t : st_h, st_b, st_l};
+    const cuuint32_t box[5] = {64, (cuuint32_t)(queries ? heads : tokens), (cuuint32_t)(queries ? tokens : 1), 1, 1}, each[5] = {1, 1, 1, 1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void *>(ptr), dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+inline bool chunk_pot_map(TcEncodeFn encode, CUtensorMap *map, const void *ptr, const ChunkParams &p, int pot_units, int keys)
+{
+    const cuuint64_t dims[3] = {(cuuint64_t)p.d, (cuuint64_t)(p.len > 0 ? p.len : 1), (cuuint64_t)pot_units};
+    const cuuint64_t strides[2] = {(cuuint64_t)p.d * 2, (cuuint64_t)p.unit_rows * p.d * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)keys, 1}, each[3] = {1, 1, 1};
+    return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(ptr), dims, strides, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// *done: the call has been launched (or failed to be); false: its strides are none that a tensor map takes.
+template <int D, bool kSplit>
+inline cudaError_t launch_chunk_tc_t(const ChunkParams &c, const ChunkTcHost &host, int tile_tokens, int tiles, int cluster, cudaStream_t stream, bool *done)
+{
+    using L = ChunkTc<D, kSplit>;
+    *done = false;
+    TcEncodeFn encode = (TcEncodeFn)host.encode;
+    CUtensorMap q, K, V, k, v;
+    if (!chunk_map(encode, &q, c.q, c, c.qs, c.Hkv * c.G, true, c.G, tile_tokens) || !chunk_map(encode, &k, c.k, c, c.ks, c.Hkv, false, 1, L::kKeys) ||
+        !chunk_map(encode, &v, c.v, c, c.vs, c.Hkv, false, 1, L::kKeys) || !chunk_pot_map(encode, &K, c.potK, c, host.pot_units, L::kKeys) ||
+        !chunk_pot_map(encode, &V, c.potV, c, host.pot_units, L::kKeys))
+        return cudaSuccess;
+    *done = true;
+    auto kern = chunk_tc_kernel<D, kSplit>;
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L::kSmemBytes);
+    if (e != cudaSuccess) return e;
+    ChunkTcParams p;
+    p.c = c;
+    p.tile_tokens = tile_tokens;
+    p.items_per_unit = (tiles + L::kQTiles - 1) / L::kQTiles;
+    p.merge = kSplit || cluster > 1;
+    p.withhold = host.withhold;
+    p.wait_ns = host.wait_ns;
+    p.status = c.status;
+    cudaLaunchConfig_t lc = {};
+    lc.gridDim = dim3((unsigned)cluster * p.items_per_unit * (unsigned)(c.layers * c.streams * c.Hkv));
+    lc.blockDim = dim3(L::kThreads);
+    lc.dynamicSmemBytes = L::kSmemBytes;
+    lc.stream = stream;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = cluster;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    lc.attrs = at;
+    lc.numAttrs = 2;
+    return cudaLaunchKernelEx(&lc, kern, q, K, V, k, v, p);
+}
+
+inline cudaError_t launch_chunk_tc(const ChunkParams &c, const ChunkTcHost &host, cudaStream_t stream, bool *done)
+{
+    const int tile_tokens = kCtRows / c.G, tiles = (c.n + tile_tokens - 1) / tile_tokens;
+    const long long units = (long long)c.layers * c.streams * c.Hkv;
+    // two query tiles a block share its key tiles where that leaves no SM without work
+    const bool pairs = c.d <= 128 && units * ((tiles + 1) / 2) >= host.sm_count;
+    const long long items = units * (pairs ? (tiles + 1) / 2 : tiles);
+    const int keys = c.d > 128 ? 64 : 128, key_tiles = (c.len + keys - 1) / keys + (c.n + keys - 1) / keys;
+    int cluster = 1;
+    while (!pairs && cluster < 8 && items * cluster * 2 <= host.sm_count && key_tiles >= 4 * cluster) cluster *= 2;
+    if (items * cluster > 0x7fffffff) return cudaErrorInvalidValue;
+    if (c.d > 128) return launch_chunk_tc_t<256, true>(c, host, tile_tokens, tiles, cluster, stream, done);
+    if (c.d > 64) return pairs ? launch_chunk_tc_t<128, false>(c, host, tile_tokens, tiles, cluster, stream, done)
+                               : launch_chunk_tc_t<128, true>(c, host, tile_tokens, tiles, cluster, stream, done);
+    return pairs ? launch_chunk_tc_t<64, false>(c, host, tile_tokens, tiles, cluster, stream, done)
+                 : launch_chunk_tc_t<64, true>(c, host, tile_tokens, tiles, cluster, stream, done);
+}
+
+}  // namespace ipotk

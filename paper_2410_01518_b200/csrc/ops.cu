@@ -3,6 +3,7 @@
 
 #include "k_blocks.cuh"
 #include "k_chunk_fma.cuh"
+#include "k_chunk_tc.cuh"
 #include "k_rotary.cuh"
 
 namespace ipotk {
@@ -25,9 +26,19 @@ cudaError_t launch_rope_rows(const RopeRowsParams &p, bool f32, bool table_f32, 
     return interleaved ? launch_rope_rows_t<bf16, bf16, true>(p, stream) : launch_rope_rows_t<bf16, bf16, false>(p, stream);
 }
 
-cudaError_t launch_chunk_attention(const ChunkParams &p, bool f32, cudaStream_t stream)
+// Tensor cores for bf16, unless a group's heads do not fit into one tile of query rows or the strides are none that a tensor map
+// takes (an input whose rows repeat by a stride of 0).
+cudaError_t launch_chunk_attention(const ChunkParams &p, bool f32, const ChunkTcHost &host, cudaStream_t stream)
 {
-    return f32 ? launch_chunk_fma<float>(p, stream) : launch_chunk_fma<__nv_bfloat16>(p, stream);
+    if (f32) return launch_chunk_fma<float>(p, stream);
+    if (host.encode && p.G <= kCtRows) {
+        bool done = false;
+        ChunkParams t = p;
+        t.scale_log2e = tensor_scale_log2e(p.d);
+        const cudaError_t e = launch_chunk_tc(t, host, stream, &done);
+        if (done || e != cudaSuccess) return e;
+    }
+    return launch_chunk_fma<__nv_bfloat16>(p, stream);
 }
 
 cudaError_t launch_block_bounds(const void *K, void *lo, void *hi, int first_row, int len, int rows, int d, int units, size_t unit_rows, int unit_blocks, bool f32,

@@ -48,8 +48,24 @@ struct ChunkParams {
     int unit_rows, len;
     int layers, streams, Hkv, G, d, n;
     float scale_log2e;
+    int *status;
 };
-cudaError_t launch_chunk_attention(const ChunkParams &p, bool f32, cudaStream_t stream);
+// What the tensor-core kernel needs besides.
+struct ChunkTcHost {
+    void *encode;                  // cuTensorMapEncodeTiled, or NULL: no tensor-core kernel
+    int sm_count, pot_units;
+    int withhold;                  // -1; test hook: this stream's softmax never reports
+    unsigned long long wait_ns;
+};
+struct ChunkTcParams {
+    ChunkParams c;
+    int tile_tokens, items_per_unit;
+    bool merge;
+    int withhold;
+    unsigned long long wait_ns;
+    int *status;
+};
+cudaError_t launch_chunk_attention(const ChunkParams &p, bool f32, const ChunkTcHost &host, cudaStream_t stream);
 
 // ------------------------------------------------------------------ generation over selected blocks (k_blocks.cuh)
 struct BlocksParams {
