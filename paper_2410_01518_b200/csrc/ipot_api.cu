@@ -1215,12 +1215,14 @@ int ipot_decode_attention_blocks(ipot_t *p, int layer, int n_layers, const void 
     if (!device.ok) return IPOT_E_CUDA;
     int rc = materialise(p, true, true);
     if (rc != IPOT_OK) return rc;
-    BlocksParams b;
+    FewParams b = {};
     b.q = q; b.K = score_keys(p); b.V = p->V; b.lo = p->blk_lo; b.hi = p->blk_hi;
+    row_strides(p, nullptr, p->cfg.Hq, 1, b.qs);
+    b.os = b.qs;
     b.out = out; b.lse = lse; b.list = blocks;
     b.unit0 = layer * p->cfg.batch * p->cfg.Hkv;
-    b.unit_rows = p->cfg.pot_size; b.unit_blocks = p->blk_count; b.len = p->len; b.rows = p->blk_rows; b.blocks = n_blocks;
-    b.layers = n_layers; b.streams = p->cfg.batch; b.Hkv = p->cfg.Hkv; b.G = p->G; b.d = p->cfg.d;
+    b.unit_rows = p->cfg.pot_size; b.unit_blocks = p->blk_count; b.len = p->len; b.block_rows = p->blk_rows; b.blocks = n_blocks;
+    b.n = 1; b.layers = n_layers; b.streams = p->cfg.batch; b.Hkv = p->cfg.Hkv; b.G = p->G; b.d = p->cfg.d;
     b.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)p->cfg.d));
     IPOT_CUDA(launch_decode_blocks(b, p->cfg.dtype == IPOT_F32, p->sm_count, p->stream));
     p->launches += 1;

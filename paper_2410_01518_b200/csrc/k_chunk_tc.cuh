@@ -17,8 +17,8 @@
 // raises the block's give-up flag and IPOT_E_TIMEOUT; from then on nothing more is put in flight, and what is in flight is
 // waited for before tensor memory is released.
 #pragma once
-#include "k_blocks.cuh"   // cluster_*
 #include "k_chunk_fma.cuh"
+#include "k_few.cuh"   // cluster_*
 #include "ops.h"
 #include "ptx.cuh"
 

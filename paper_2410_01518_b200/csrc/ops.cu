@@ -4,6 +4,7 @@
 #include "k_blocks.cuh"
 #include "k_chunk_fma.cuh"
 #include "k_chunk_tc.cuh"
+#include "k_few.cuh"
 #include "k_rotary.cuh"
 
 namespace ipotk {
@@ -26,10 +27,20 @@ cudaError_t launch_rope_rows(const RopeRowsParams &p, bool f32, bool table_f32, 
     return interleaved ? launch_rope_rows_t<bf16, bf16, true>(p, stream) : launch_rope_rows_t<bf16, bf16, false>(p, stream);
 }
 
-// Tensor cores for bf16, unless a group's heads do not fit into one tile of query rows or the strides are none that a tensor map
+// Few rows have a kernel of their own; else tensor cores for bf16, unless a group's heads do not fit into one tile of query rows or the strides are none that a tensor map
 // takes (an input whose rows repeat by a stride of 0).
 cudaError_t launch_chunk_attention(const ChunkParams &p, bool f32, const ChunkTcHost &host, cudaStream_t stream)
 {
+    if (p.n * p.G <= kFewRows) {
+        FewParams f = {};
+        f.q = p.q; f.qs = p.qs; f.K = p.potK; f.V = p.potV;
+        f.unit0 = p.unit0; f.unit_rows = p.unit_rows; f.len = p.len;
+        f.k = p.k; f.v = p.v; f.ks = p.ks; f.vs = p.vs; f.tokens = p.tokens; f.n = p.n;
+        f.out = p.out; f.os = p.os; f.lse = p.lse;
+        f.layers = p.layers; f.streams = p.streams; f.Hkv = p.Hkv; f.G = p.G; f.d = p.d;
+        f.scale_log2e = p.scale_log2e;
+        return launch_few<false>(f, f32, host.sm_count, stream);
+    }
     if (f32) return launch_chunk_fma<float>(p, stream);
     if (host.encode && p.G <= kCtRows) {
         bool done = false;
@@ -48,14 +59,9 @@ cudaError_t launch_block_bounds(const void *K, void *lo, void *hi, int first_row
                : launch_block_bounds_t<__nv_bfloat16>(K, lo, hi, first_row, len, rows, d, units, unit_rows, unit_blocks, stream);
 }
 
-cudaError_t launch_decode_blocks(const BlocksParams &p, bool f32, int sm_count, cudaStream_t stream)
+cudaError_t launch_decode_blocks(const FewParams &p, bool f32, int sm_count, cudaStream_t stream)
 {
-    // blocks of a cluster: enough for every SM to have one or two, and none without a few dozen rows
-    const long long units = (long long)p.layers * p.streams * p.Hkv * ((p.G + kBlkHeads - 1) / kBlkHeads);
-    const int rows = p.blocks < (p.len + p.rows - 1) / p.rows ? p.blocks * p.rows : p.len;
-    int cluster = 1;
-    while (cluster < 8 && units * cluster * 2 <= 2LL * sm_count && rows / cluster >= 64) cluster *= 2;
-    return f32 ? launch_blocks<float>(p, cluster, stream) : launch_blocks<__nv_bfloat16>(p, cluster, stream);
+    return launch_few<true>(p, f32, sm_count, stream);
 }
 
 }  // namespace ipotk

@@ -67,18 +67,28 @@ struct ChunkTcParams {
 };
 cudaError_t launch_chunk_attention(const ChunkParams &p, bool f32, const ChunkTcHost &host, cudaStream_t stream);
 
-// ------------------------------------------------------------------ generation over selected blocks (k_blocks.cuh)
-struct BlocksParams {
-    const void *q;                 // [layers][streams][Hkv * G][d]
+// ------------------------------------------------------------------ few query rows, generation over selected blocks (k_few.cuh, k_blocks.cuh)
+struct FewParams {
+    const void *q;                 // of the layers asked for
+    Strides qs;
     const void *K, *V;             // [units][unit_rows][d], from the pot's first unit on
+    int unit0, unit_rows, len;
+    // a chunk of few tokens (1 token and none of these over selected blocks)
+    const void *k, *v;
+    Strides ks, vs;
+    const int32_t *tokens;
+    int n;
+    // selected blocks
     const void *lo, *hi;           // [units][unit_blocks][d]
-    float *out, *lse;              // of the layers asked for
     int32_t *list;                 // [layers][streams][Hkv][blocks], or NULL
-    int unit0, unit_rows, unit_blocks, len, rows, blocks;
+    int unit_blocks, block_rows, blocks;
+    void *out;
+    Strides os;
+    float *lse;                    // [layers][streams][heads][n], or NULL
     int layers, streams, Hkv, G, d;
     float scale_log2e;
 };
-cudaError_t launch_decode_blocks(const BlocksParams &p, bool f32, int sm_count, cudaStream_t stream);
+cudaError_t launch_decode_blocks(const FewParams &p, bool f32, int sm_count, cudaStream_t stream);
 // bounds of the blocks that hold rows [first_row, len) of every unit
 cudaError_t launch_block_bounds(const void *K, void *lo, void *hi, int first_row, int len, int rows, int d, int units, size_t unit_rows, int unit_blocks, bool f32,
                                 cudaStream_t stream);
