@@ -364,9 +364,9 @@ typedef struct {
  *   rope     : the tables [rows][rotary_dim / 2], 16-byte aligned, of type dtype (need not be the pot's); pairing as for
  *              ipot_enable_rope, within the first rotary_dim channels
  * In place (q_out == q with equal strides) is allowed; other overlaps of inputs and outputs are not.  `layers` is that of the arrays,
- * any number up to 65535.  Asynchronous on the pot's stream; the pot's contents are neither read nor changed.
+ * any number with layers * batch up to 65535.  Asynchronous on the pot's stream; the pot's contents are neither read nor changed.
  * Errors: INVALID (NULL, misaligned, sizes, strides, rotary_dim odd, < 2 or > d, first outside the table, in place with other strides;
- * n_tokens so large that a stream's work items pass 2^31), CUDA.
+ * n_tokens * d of 2^31 or more), CUDA.
  */
 typedef struct {
     const void *cos_table, *sin_table;

@@ -1108,7 +1108,7 @@ int ipot_rope_rows(ipot_t *p, const ipot_rope_t *rope, int layers, int n, const 
 {
     if (!p || !rope || !rope->cos_table || !rope->sin_table || !aligned16(rope->cos_table) || !aligned16(rope->sin_table)) return IPOT_E_INVALID;
     if (!q != !q_out || !k != !k_out || (!q && !k)) return IPOT_E_INVALID;
-    if (layers < 1 || layers > 65535 || p->cfg.batch > 65535 || n < 1) return IPOT_E_INVALID;
+    if (layers < 1 || (long long)layers * p->cfg.batch > 65535 || n < 1) return IPOT_E_INVALID;
     if (rope->dtype != IPOT_BF16 && rope->dtype != IPOT_F32) return IPOT_E_INVALID;
     if (rope->pairing != IPOT_ROPE_HALF && rope->pairing != IPOT_ROPE_INTERLEAVED) return IPOT_E_INVALID;
     if (rope->rows < 1 || rope->rotary_dim < 2 || rope->rotary_dim % 2 || rope->rotary_dim > p->cfg.d) return IPOT_E_INVALID;
@@ -1126,7 +1126,7 @@ int ipot_rope_rows(ipot_t *p, const ipot_rope_t *rope, int layers, int n, const 
             return IPOT_E_INVALID;
         if (r.src[i] == r.dst[i] && memcmp(&r.in[i], &r.out[i], sizeof(Strides))) return IPOT_E_INVALID;
     }
-    if ((long long)n * p->cfg.d * ((p->cfg.Hq + p->cfg.Hkv + 3) / 4) >= (1LL << 31)) return IPOT_E_INVALID;
+    if ((long long)n * p->cfg.d >= (1LL << 31) || p->cfg.Hq > 65535) return IPOT_E_INVALID;
     r.cos_t = rope->cos_table; r.sin_t = rope->sin_table; r.positions = positions;
     r.first = first; r.table_rows = rope->rows; r.rotary = rope->rotary_dim;
     r.d = p->cfg.d; r.n = n; r.streams = p->cfg.batch; r.layers = layers; r.status = p->status;

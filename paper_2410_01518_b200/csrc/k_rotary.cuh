@@ -88,118 +88,107 @@ __device__ __forceinline__ void rotate_pair(float lo, float hi, float cs, float 
 
 constexpr int kRowHeads = 4;   // of a thread
 
-// Heads are numbered through queries and keys; a thread has up to kRowHeads of them, those of its group.
+// What a thread block has: a layer, a stream and up to kRowHeads neighbouring heads of the queries or of the keys; a thread has a token of
+// them (everything but the token is the block's, so addresses cost a thread one multiplication each).
 struct RowHeads {
-    const char *src[kRowHeads];
-    char *dst[kRowHeads];
-    int n;
-    __device__ __forceinline__ RowHeads(const RopeRowsParams &p, int group, int l, int b, int t, int elem)
+    const char *src;
+    char *dst;
+    long long in_head, out_head, in_token, out_token;   // bytes
+    int b, n;
+    __device__ __forceinline__ RowHeads(const RopeRowsParams &p, int elem)
     {
-        n = 0;
-        const int all = p.heads[0] + p.heads[1];
-#pragma unroll
-        for (int i = 0; i < kRowHeads; ++i) {
-            const int h = group * kRowHeads + i;
-            if (h < all) {
-                const int w = h >= p.heads[0], hh = h - (w ? p.heads[0] : 0);
-                const Strides &in = p.in[w], &out = p.out[w];
-                src[i] = (const char *)p.src[w] + (l * in.layer + b * in.stream + hh * in.head + t * in.token) * elem;
-                dst[i] = (char *)p.dst[w] + (l * out.layer + b * out.stream + hh * out.head + t * out.token) * elem;
-                n = i + 1;
-            }
-        }
+        const int q_groups = (p.heads[0] + kRowHeads - 1) / kRowHeads, group = blockIdx.y, w = group >= q_groups, h = (group - (w ? q_groups : 0)) * kRowHeads, l = blockIdx.z / p.streams;
+        b = blockIdx.z - l * p.streams;
+        const Strides &in = p.in[w], &out = p.out[w];
+        src = (const char *)p.src[w] + (l * in.layer + b * in.stream + h * in.head) * elem;
+        dst = (char *)p.dst[w] + (l * out.layer + b * out.stream + h * out.head) * elem;
+        in_head = in.head * elem;
+        out_head = out.head * elem;
+        in_token = in.token * elem;
+        out_token = out.token * elem;
+        n = min(kRowHeads, p.heads[w] - h);
     }
 };
 
-// grid (blocks over tokens x head groups x items, streams, layers).  Items of a row: half pairing, one per vector of the lower
-// half (it brings its partner); interleaved, one per rotated vector; and one per vector that is copied.
+// grid (blocks over tokens x items, head groups, layers x streams).  Items of a row: half pairing, one per vector of the lower
+// half (it brings its partner); interleaved, one per rotated vector; and one per vector, or two vectors, that are copied.  Both kinds load before
+// and store behind the rotation: a warp has items of both.
 template <typename T, typename TT, bool kInterleaved>
 __global__ void __launch_bounds__(kRotThreads)
-rope_rows_kernel(const __grid_constant__ RopeRowsParams p, int items, int groups)
+rope_rows_kernel(const __grid_constant__ RopeRowsParams p, int items)
 {
     pdl_wait();
     pdl_release();
     constexpr int VE = RowVec<T>::kElems;
-    const unsigned at = blockIdx.x * kRotThreads + threadIdx.x;
-    const unsigned per_token = (unsigned)(items * groups), t = at / per_token, rest = at - t * per_token;
+    const unsigned at = blockIdx.x * kRotThreads + threadIdx.x, t = at / (unsigned)items;
     if (t >= (unsigned)p.n) return;
-    const int group = rest / items, item = rest - group * items, b = blockIdx.y, l = blockIdx.z;
-    const int pos = rope_position(p, b, t);
+    const int item = at - t * items;
+    const RowHeads rows(p, sizeof(T));
+    const int pos = rope_position(p, rows.b, t);
     if (pos < 0) return;
-    const int rv = p.rotary / VE, half = p.rotary / 2, turned = kInterleaved ? rv : rv / 2;
-    const RowHeads rows(p, group, l, b, t, sizeof(T));
+    const char *src = rows.src + t * rows.in_token;
+    char *dst = rows.dst + t * rows.out_token;
+    // its vector, and (half pairing) a second one: the partner, or where vectors are copied one more of them
+    const int rv = p.rotary / VE, half = p.rotary / 2, turned = kInterleaved ? rv : rv / 2, vecs = p.d / VE;
+    const bool turns = item < turned;
+    const int v = turns ? item : rv + item - turned, v2 = turns ? item + turned : v + (vecs - rv + 1) / 2;
+    const bool two = !kInterleaved && v2 < vecs;
     RowVec<T> x[kRowHeads], y[kRowHeads];
-    if (item >= turned) {   // a vector behind the rotated part
-        const int v = rv + item - turned;
 #pragma unroll
-        for (int i = 0; i < kRowHeads; ++i)
-            if (i < rows.n) x[i] = reinterpret_cast<const RowVec<T> *>(rows.src[i])[v];
-#pragma unroll
-        for (int i = 0; i < kRowHeads; ++i)
-            if (i < rows.n) reinterpret_cast<RowVec<T> *>(rows.dst[i])[v] = x[i];
-        return;
-    }
-    constexpr int TE = kInterleaved ? VE / 2 : VE;   // table entries
-    float cs[TE], sn[TE];
-    {
-        const TT *c = (const TT *)p.cos_t + (size_t)pos * half + item * TE, *s = (const TT *)p.sin_t + (size_t)pos * half + item * TE;
+    for (int i = 0; i < kRowHeads; ++i)
+        if (i < rows.n) {
+            x[i] = reinterpret_cast<const RowVec<T> *>(src + i * rows.in_head)[v];
+            if (two) y[i] = reinterpret_cast<const RowVec<T> *>(src + i * rows.in_head)[v2];
+        }
+    if (turns) {
+        constexpr int TE = kInterleaved ? VE / 2 : VE;   // table entries
         struct alignas(TE * sizeof(TT) < 16 ? TE * sizeof(TT) : 16) Part {
             TT e[TE];
         };
-        const Part pc = *reinterpret_cast<const Part *>(c), ps = *reinterpret_cast<const Part *>(s);
+        const Part pc = *reinterpret_cast<const Part *>((const TT *)p.cos_t + (size_t)pos * half + item * TE);
+        const Part ps = *reinterpret_cast<const Part *>((const TT *)p.sin_t + (size_t)pos * half + item * TE);
 #pragma unroll
         for (int k = 0; k < TE; ++k) {
-            cs[k] = to_float(pc.e[k]);
-            sn[k] = to_float(ps.e[k]);
+            const float cs = to_float(pc.e[k]), sn = to_float(ps.e[k]);
+            float a, c;
+#pragma unroll
+            for (int i = 0; i < kRowHeads; ++i) {
+                T &lo = kInterleaved ? x[i].e[2 * k] : x[i].e[k], &hi = kInterleaved ? x[i].e[2 * k + 1] : y[i].e[k];
+                rotate_pair(to_float(lo), to_float(hi), cs, sn, a, c);
+                lo = from_float<T>(a);
+                hi = from_float<T>(c);
+            }
         }
     }
 #pragma unroll
     for (int i = 0; i < kRowHeads; ++i)
         if (i < rows.n) {
-            x[i] = reinterpret_cast<const RowVec<T> *>(rows.src[i])[item];
-            if (!kInterleaved) y[i] = reinterpret_cast<const RowVec<T> *>(rows.src[i])[item + turned];
-        }
-#pragma unroll
-    for (int i = 0; i < kRowHeads; ++i)
-        if (i < rows.n) {
-            float a, c;
-#pragma unroll
-            for (int k = 0; k < TE; ++k) {
-                if (kInterleaved) {
-                    rotate_pair(to_float(x[i].e[2 * k]), to_float(x[i].e[2 * k + 1]), cs[k], sn[k], a, c);
-                    x[i].e[2 * k] = from_float<T>(a);
-                    x[i].e[2 * k + 1] = from_float<T>(c);
-                } else {
-                    rotate_pair(to_float(x[i].e[k]), to_float(y[i].e[k]), cs[k], sn[k], a, c);
-                    x[i].e[k] = from_float<T>(a);
-                    y[i].e[k] = from_float<T>(c);
-                }
-            }
-            reinterpret_cast<RowVec<T> *>(rows.dst[i])[item] = x[i];
-            if (!kInterleaved) reinterpret_cast<RowVec<T> *>(rows.dst[i])[item + turned] = y[i];
+            reinterpret_cast<RowVec<T> *>(dst + i * rows.out_head)[v] = x[i];
+            if (two) reinterpret_cast<RowVec<T> *>(dst + i * rows.out_head)[v2] = y[i];
         }
 }
 
 // Rotated parts that do not split into whole vectors: a thread has one channel pair, or one channel that is copied.
 template <typename T, typename TT, bool kInterleaved>
 __global__ void __launch_bounds__(kRotThreads)
-rope_pairs_kernel(const __grid_constant__ RopeRowsParams p, int items, int groups)
+rope_pairs_kernel(const __grid_constant__ RopeRowsParams p, int items)
 {
     pdl_wait();
     pdl_release();
-    const unsigned at = blockIdx.x * kRotThreads + threadIdx.x;
-    const unsigned per_token = (unsigned)(items * groups), t = at / per_token, rest = at - t * per_token;
+    const unsigned at = blockIdx.x * kRotThreads + threadIdx.x, t = at / (unsigned)items;
     if (t >= (unsigned)p.n) return;
-    const int group = rest / items, item = rest - group * items, b = blockIdx.y, l = blockIdx.z;
-    const int pos = rope_position(p, b, t);
+    const int item = at - t * items;
+    const RowHeads rows(p, sizeof(T));
+    const int pos = rope_position(p, rows.b, t);
     if (pos < 0) return;
+    const char *src = rows.src + t * rows.in_token;
+    char *dst = rows.dst + t * rows.out_token;
     const int half = p.rotary / 2;
-    const RowHeads rows(p, group, l, b, t, sizeof(T));
     if (item >= half) {
         const int c = p.rotary + item - half;
 #pragma unroll
         for (int i = 0; i < kRowHeads; ++i)
-            if (i < rows.n) ((T *)rows.dst[i])[c] = ((const T *)rows.src[i])[c];
+            if (i < rows.n) ((T *)(dst + i * rows.out_head))[c] = ((const T *)(src + i * rows.in_head))[c];
         return;
     }
     const float cs = to_float(((const TT *)p.cos_t)[(size_t)pos * half + item]), sn = to_float(((const TT *)p.sin_t)[(size_t)pos * half + item]);
@@ -208,9 +197,9 @@ rope_pairs_kernel(const __grid_constant__ RopeRowsParams p, int items, int group
     for (int i = 0; i < kRowHeads; ++i)
         if (i < rows.n) {
             float a, c;
-            rotate_pair(to_float(((const T *)rows.src[i])[lo]), to_float(((const T *)rows.src[i])[hi]), cs, sn, a, c);
-            ((T *)rows.dst[i])[lo] = from_float<T>(a);
-            ((T *)rows.dst[i])[hi] = from_float<T>(c);
+            rotate_pair(to_float(((const T *)(src + i * rows.in_head))[lo]), to_float(((const T *)(src + i * rows.in_head))[hi]), cs, sn, a, c);
+            ((T *)(dst + i * rows.out_head))[lo] = from_float<T>(a);
+            ((T *)(dst + i * rows.out_head))[hi] = from_float<T>(c);
         }
 }
 
@@ -220,12 +209,12 @@ inline cudaError_t launch_rope_rows_t(const RopeRowsParams &p, cudaStream_t stre
     constexpr int VE = RowVec<T>::kElems;
     // whole vectors: of the rows, and (half pairing) of each half of the rotated part
     const bool vectors = p.rotary % (kInterleaved ? VE : 2 * VE) == 0;
-    const int items = vectors ? p.d / VE - (kInterleaved ? 0 : p.rotary / VE / 2) : p.d - p.rotary / 2;
-    const int groups = (p.heads[0] + p.heads[1] + kRowHeads - 1) / kRowHeads;
-    const long long threads = (long long)p.n * items * groups;
-    const dim3 grid((unsigned)((threads + kRotThreads - 1) / kRotThreads), p.streams, p.layers);
-    return launch_pdl(vectors ? rope_rows_kernel<T, TT, kInterleaved> : rope_pairs_kernel<T, TT, kInterleaved>, grid, dim3(kRotThreads), 0, stream, p, items,
-                      groups);
+    const int rest = p.d / VE - p.rotary / VE;   // vectors that are copied
+    const int items = vectors ? (kInterleaved ? p.d / VE : p.rotary / VE / 2 + (rest + 1) / 2) : p.d - p.rotary / 2;
+    const int groups = (p.heads[0] + kRowHeads - 1) / kRowHeads + (p.heads[1] + kRowHeads - 1) / kRowHeads;
+    const long long threads = (long long)p.n * items;
+    const dim3 grid((unsigned)((threads + kRotThreads - 1) / kRotThreads), groups, p.layers * p.streams);
+    return launch_pdl(vectors ? rope_rows_kernel<T, TT, kInterleaved> : rope_pairs_kernel<T, TT, kInterleaved>, grid, dim3(kRotThreads), 0, stream, p, items);
 }
 
 }  // namespace ipotk
