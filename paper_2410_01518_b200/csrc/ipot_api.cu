@@ -182,11 +182,25 @@ int update_blocks(ipot *p, int first_row, int len)
     return IPOT_OK;
 }
 
+// An append, K and V [units][n][d] behind slot first, that takes the bounds of the blocks along.
+int append_with_blocks(ipot *p, const void *K, const void *V, int first, int n)
+{
+    IPOT_CUDA(launch_append_bounds(K, V, p->K, p->V, p->blk_lo, p->blk_hi, first, n, p->blk_rows, p->cfg.d, p->units, p->cfg.pot_size, p->blk_count,
+                                   p->cfg.dtype == IPOT_F32, p->sm_count, p->stream));
+    p->launches += 1;
+    return IPOT_OK;
+}
+
 // Copies the rows of a deferred append that are still in the caller's buffers into the pot (keys, values or both).
 int materialise(ipot *p, bool keys, bool values)
 {
     const void *k = keys ? p->pend_K : nullptr, *v = values ? p->pend_V : nullptr;
     if (!k && !v) return IPOT_OK;
+    if (k && v && p->blk_rows && !p->rope) {
+        int rc = append_with_blocks(p, k, v, p->pend_first, p->pend_n);
+        if (rc == IPOT_OK) p->pend_K = p->pend_V = nullptr;
+        return rc;
+    }
     const size_t row_vecs = p->row_bytes / 16, n_vecs = (size_t)p->pend_n * row_vecs;
     int pieces = (int)((n_vecs + (size_t)kMoveThreads * kMoveVecs - 1) / ((size_t)kMoveThreads * kMoveVecs));
     if (pieces < 1) pieces = 1;
@@ -909,6 +923,11 @@ int ipot_append_chunk(ipot_t *p, const void *K, const void *V, int n)
         }
         p->len += n;
         return p->rope ? update_blocks(p, p->len - n, p->len) : IPOT_OK;   // (else the keys are not in the pot yet)
+    }
+    if (!p->rope && p->blk_rows) {
+        rc = append_with_blocks(p, K, V, p->len, n);
+        if (rc == IPOT_OK) p->len += n;
+        return rc;
     }
     if (!p->rope) {
         dim3 grid(pieces, p->units, 2);

@@ -59,6 +59,13 @@ cudaError_t launch_block_bounds(const void *K, void *lo, void *hi, int first_row
                : launch_block_bounds_t<__nv_bfloat16>(K, lo, hi, first_row, len, rows, d, units, unit_rows, unit_blocks, stream);
 }
 
+cudaError_t launch_append_bounds(const void *srcK, const void *srcV, void *potK, void *potV, void *lo, void *hi, int first_row, int n, int rows, int d, int units, size_t unit_rows,
+                                 int unit_blocks, bool f32, int sm_count, cudaStream_t stream)
+{
+    return f32 ? launch_append_bounds_t<float>(srcK, srcV, potK, potV, lo, hi, first_row, n, rows, d, units, unit_rows, unit_blocks, sm_count, stream)
+               : launch_append_bounds_t<__nv_bfloat16>(srcK, srcV, potK, potV, lo, hi, first_row, n, rows, d, units, unit_rows, unit_blocks, sm_count, stream);
+}
+
 cudaError_t launch_decode_blocks(const FewParams &p, bool f32, int sm_count, cudaStream_t stream)
 {
     return launch_few<true>(p, f32, sm_count, stream);

@@ -93,4 +93,8 @@ cudaError_t launch_decode_blocks(const FewParams &p, bool f32, int sm_count, cud
 cudaError_t launch_block_bounds(const void *K, void *lo, void *hi, int first_row, int len, int rows, int d, int units, size_t unit_rows, int unit_blocks, bool f32,
                                 cudaStream_t stream);
 
+// an append of n rows of keys and values [units][n][d] behind first_row, bounds included
+cudaError_t launch_append_bounds(const void *srcK, const void *srcV, void *potK, void *potV, void *lo, void *hi, int first_row, int n, int rows, int d, int units, size_t unit_rows,
+                                 int unit_blocks, bool f32, int sm_count, cudaStream_t stream);
+
 }  // namespace ipotk
