@@ -1,28 +1,29 @@
-// Attention of a chunk of new tokens over the pot and, causally, over itself, with fp32 FMAs: every type, head dimension and
-// group size.  out_h[t] = sum_j softmax_j(q_h[t] . k_j / sqrt(d)) v_j over the pot's rows [0, len) and the chunk's rows 0 .. t.
+// Attention of a chunk of new tokens over the pot and, causally, over itself, with fp32 FMAs: f32 pots, and bf16 calls that the tensor-core
+// kernel does not take.  out_h[t] = sum_j softmax_j(q_h[t] . k_j / sqrt(d)) v_j over the pot's rows [0, len) and the chunk's rows 0 .. t.
 //
-// The query heads of a KV head share its keys, so a unit's rows are folded token by token: row t * G + g.  A block has BM of
-// them and goes over the keys they see in tiles of 64, with the running maximum and sum of the softmax: products S = Q K^T from
-// transposed tiles in shared memory (a thread has BM / 16 rows x 4 keys), probabilities back into shared memory, O += P V with BM / 16 rows
-// x d / 16 channels in a thread's registers.  Everything is fp32.  Bound: FMA issue and shared-memory reads (4 x 4 products
-// per two 16-byte reads).
+// The query heads of a KV head share its keys, so a unit's rows are folded token by token: row t * G + g.  A block has 64 of
+// them and goes over the keys they see in tiles of 64, with the running maximum and sum of the softmax.  A thread has 4 rows x 4 keys of S = Q K^T, summed over
+// pairs of channels with packed FMAs from rows as they lie in memory (pitches keep the 16-byte reads free of bank conflicts), and 4 rows x
+// d / 16 channels of O += P V in registers; P goes through shared memory.  Few row tiles spread their keys over a cluster, whose blocks merge through distributed shared
+// memory.  Bound: FMA issue and shared-memory reads (32 packed FMAs per eight 16-byte reads).
 #pragma once
 #include "common.cuh"
 #include "ops.h"
+#include "cluster.cuh"
 #include "k_rotary.cuh"   // RowVec, to_float, from_float
 
 namespace ipotk {
 
 constexpr int kCfThreads = 256;
-constexpr int kCfKeys = 64;
+constexpr int kCfRows = 64, kCfKeys = 64;
 
-template <int DP, int BM> struct ChunkFmaSmem {
-    static constexpr int kKeyPitch = kCfKeys + 4;   // (the transposing stores of a warp then fall into different banks)
-    static constexpr int kRowPitch = BM + 4;
-    float q[DP][kRowPitch];
-    float k[DP][kKeyPitch];
-    float v[kCfKeys][DP];
-    float p[kCfKeys][kRowPitch];
+template <int DP> struct ChunkFmaSmem {
+    static constexpr int kPitch = DP + 4, kPPitch = kCfKeys + 16;
+    float q[kCfRows][kPitch];
+    float k[kCfKeys][kPitch];   // keys and values of a tile; at the end the block's partial result
+    float v[kCfKeys][kPitch];
+    float p[kCfRows][kPPitch];
+    float2 stat[kCfRows];
 };
 
 __device__ __forceinline__ float chunk_ex2(float x)
@@ -35,87 +36,100 @@ __device__ __forceinline__ float chunk_ex2(float x)
 // Tokens of stream b that are there.
 __device__ __forceinline__ int chunk_tokens(const ChunkParams &p, int b) { return p.tokens ? min(max(__ldg(p.tokens + b), 0), p.n) : p.n; }
 
-template <typename T, int DP, int BM>
+// grid: cluster x (row tiles, the longest first) x units.
+template <typename T, int DP>
 __global__ void __launch_bounds__(kCfThreads)
-chunk_fma_kernel(const __grid_constant__ ChunkParams p)
+chunk_fma_kernel(const __grid_constant__ ChunkParams p, int units)
 {
     pdl_wait();
     pdl_release();
-    using Smem = ChunkFmaSmem<DP, BM>;
-    constexpr int VE = RowVec<T>::kElems, RT = BM / 16, CV = DP / 64;   // rows and 4-channel vectors of a thread
+    using Smem = ChunkFmaSmem<DP>;
+    constexpr int VE = RowVec<T>::kElems, CV = DP / 64;   // 4-channel vectors of a thread
     extern __shared__ __align__(16) uint8_t chunk_raw[];
     Smem &sm = *reinterpret_cast<Smem *>(chunk_raw);
-    const int unit = blockIdx.y, hkv = unit % p.Hkv, b = unit / p.Hkv % p.streams, l = unit / p.Hkv / p.streams;
-    const int n = chunk_tokens(p, b), G = p.G, row0 = ((int)gridDim.x - 1 - (int)blockIdx.x) * BM;   // the longest rows first
-    if (row0 >= n * G) return;
-    const int rows = min(BM, n * G - row0), keys = p.len + (row0 + rows - 1) / G + 1;
+    const uint32_t rank = cluster_rank(), ranks = cluster_size();
+    const int item = blockIdx.x / ranks, items = gridDim.x / ranks, unit = item % units, hkv = unit % p.Hkv, b = unit / p.Hkv % p.streams, l = unit / p.Hkv / p.streams;
+    const int n = chunk_tokens(p, b), G = p.G, row0 = (items / units - 1 - item / units) * kCfRows;
+    if (row0 >= n * G) return;   // (the whole cluster)
+    const int rows = min(kCfRows, n * G - row0), all_keys = p.len + (row0 + rows - 1) / G + 1, tiles = (all_keys + kCfKeys - 1) / kCfKeys;
+    const int first = (int)((long long)tiles * rank / ranks) * kCfKeys, keys = min(all_keys, (int)((long long)tiles * (rank + 1) / ranks) * kCfKeys);
     const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, vecs = p.d / VE;
     const T *potK = (const T *)p.potK + (size_t)(p.unit0 + unit) * p.unit_rows * p.d, *potV = (const T *)p.potV + (size_t)(p.unit0 + unit) * p.unit_rows * p.d;
     const T *newK = (const T *)p.k + l * p.ks.layer + b * p.ks.stream + hkv * p.ks.head, *newV = (const T *)p.v + l * p.vs.layer + b * p.vs.stream + hkv * p.vs.head;
     const T *q = (const T *)p.q + l * p.qs.layer + b * p.qs.stream + (long long)hkv * G * p.qs.head;
 
-    if (DP > p.d) {   // channels that are not there count as zeros
-        for (int i = tid; i < (DP - p.d) * Smem::kRowPitch; i += kCfThreads) sm.q[p.d][i] = 0.f;
-        for (int i = tid; i < (DP - p.d) * Smem::kKeyPitch; i += kCfThreads) sm.k[p.d][i] = 0.f;
-        for (int i = tid; i < kCfKeys * (DP - p.d); i += kCfThreads) sm.v[i / (DP - p.d)][p.d + i % (DP - p.d)] = 0.f;
+    // channels that are not there count as zeros
+    for (int i = tid; i < kCfRows * (DP - p.d); i += kCfThreads) {
+        const int r = i / (DP - p.d), c = p.d + i - r * (DP - p.d);
+        sm.q[r][c] = sm.k[r][c] = sm.v[r][c] = 0.f;
     }
-    for (int i = tid; i < BM * vecs; i += kCfThreads) {
-        const int r = i % BM, v = i / BM, t = (row0 + r) / G, g = row0 + r - t * G;
+    auto put = [&](float *dst, const T *src, bool there, float scale) {   // a vector, as floats; zeros where there is none
         RowVec<T> x;
-        if (r < rows) x = *reinterpret_cast<const RowVec<T> *>(q + (long long)t * p.qs.token + g * p.qs.head + v * VE);
+        if (there) x = *reinterpret_cast<const RowVec<T> *>(src);
 #pragma unroll
-        for (int e = 0; e < VE; ++e) sm.q[v * VE + e][r] = r < rows ? to_float(x.e[e]) * p.scale_log2e : 0.f;
+        for (int e = 0; e < VE; e += 4)
+            *reinterpret_cast<float4 *>(dst + e) = there ? make_float4(to_float(x.e[e]) * scale, to_float(x.e[e + 1]) * scale, to_float(x.e[e + 2]) * scale, to_float(x.e[e + 3]) * scale)
+                                                         : make_float4(0.f, 0.f, 0.f, 0.f);
+    };
+    for (int i = tid; i < kCfRows * vecs; i += kCfThreads) {
+        const int r = i / vecs, v = i - r * vecs, t = (row0 + r) / G, g = row0 + r - t * G;
+        put(&sm.q[r][v * VE], q + (long long)t * p.qs.token + g * p.qs.head + v * VE, r < rows, p.scale_log2e);
     }
-    float m[RT], sum[RT], acc[RT][CV][4];
-    int limit[RT];
+    // a thread's rows are ty + 16 i, its keys tx + 16 j of a tile, its channels 64 c + 4 tx ..
+    float m[4], sum[4];
+    float4 acc[4][CV];
+    int limit[4];
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
+    for (int i = 0; i < 4; ++i) {
         m[i] = -INFINITY;
         sum[i] = 0.f;
-        limit[i] = p.len + (row0 + ty * RT + i) / G + 1;
+        limit[i] = p.len + (row0 + ty + 16 * i) / G + 1;
 #pragma unroll
-        for (int c = 0; c < CV; ++c) acc[i][c][0] = acc[i][c][1] = acc[i][c][2] = acc[i][c][3] = 0.f;
+        for (int c = 0; c < CV; ++c) acc[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
     }
-    for (int k0 = 0; k0 < keys; k0 += kCfKeys) {
+    for (int k0 = first; k0 < keys; k0 += kCfKeys) {
         __syncthreads();
-        for (int i = tid; i < kCfKeys * vecs; i += kCfThreads) {
-            const int r = i % kCfKeys, v = i / kCfKeys, j = k0 + r;
-            RowVec<T> x;
-            if (j < keys) x = *reinterpret_cast<const RowVec<T> *>((j < p.len ? potK + (size_t)j * p.d : newK + (j - p.len) * p.ks.token) + v * VE);
-#pragma unroll
-            for (int e = 0; e < VE; ++e) sm.k[v * VE + e][r] = j < keys ? to_float(x.e[e]) : 0.f;
-        }
+#pragma unroll 4
         for (int i = tid; i < kCfKeys * vecs; i += kCfThreads) {
             const int r = i / vecs, v = i - r * vecs, j = k0 + r;
-            RowVec<T> x;
-            if (j < keys) x = *reinterpret_cast<const RowVec<T> *>((j < p.len ? potV + (size_t)j * p.d : newV + (j - p.len) * p.vs.token) + v * VE);
-#pragma unroll
-            for (int e = 0; e < VE; ++e) sm.v[r][v * VE + e] = j < keys ? to_float(x.e[e]) : 0.f;
+            put(&sm.k[r][v * VE], (j < p.len ? potK + (size_t)j * p.d : newK + (j - p.len) * p.ks.token) + v * VE, j < keys, 1.f);
+            put(&sm.v[r][v * VE], (j < p.len ? potV + (size_t)j * p.d : newV + (j - p.len) * p.vs.token) + v * VE, j < keys, 1.f);
         }
         __syncthreads();
-        float s[RT][4];
+        float s[4][4];
+        {
+            float2 s2[4][4];
 #pragma unroll
-        for (int i = 0; i < RT; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s2[i][j] = make_float2(0.f, 0.f);
 #pragma unroll 4
-        for (int c = 0; c < DP; ++c) {
-            float a[RT];
-            if (RT == 4) *reinterpret_cast<float4 *>(a) = *reinterpret_cast<const float4 *>(&sm.q[c][ty * RT]);
-            else a[0] = sm.q[c][ty];
-            const float4 k4 = *reinterpret_cast<const float4 *>(&sm.k[c][tx * 4]);
+            for (int c = 0; c < DP; c += 4) {
+                float4 a[4], k4[4];
 #pragma unroll
-            for (int i = 0; i < RT; ++i) {
-                s[i][0] = fmaf(a[i], k4.x, s[i][0]);
-                s[i][1] = fmaf(a[i], k4.y, s[i][1]);
-                s[i][2] = fmaf(a[i], k4.z, s[i][2]);
-                s[i][3] = fmaf(a[i], k4.w, s[i][3]);
+                for (int i = 0; i < 4; ++i) {
+                    a[i] = *reinterpret_cast<const float4 *>(&sm.q[ty + 16 * i][c]);
+                    k4[i] = *reinterpret_cast<const float4 *>(&sm.k[tx + 16 * i][c]);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        s2[i][j] = __ffma2_rn(make_float2(a[i].x, a[i].y), make_float2(k4[j].x, k4[j].y), s2[i][j]);
+                        s2[i][j] = __ffma2_rn(make_float2(a[i].z, a[i].w), make_float2(k4[j].z, k4[j].w), s2[i][j]);
+                    }
             }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[i][j] = s2[i][j].x + s2[i][j].y;
         }
 #pragma unroll
-        for (int i = 0; i < RT; ++i) {
+        for (int i = 0; i < 4; ++i) {
             float mt = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if (k0 + tx * 4 + j >= limit[i]) s[i][j] = -INFINITY;
+                if (k0 + tx + 16 * j >= limit[i]) s[i][j] = -INFINITY;
                 mt = fmaxf(mt, s[i][j]);
             }
 #pragma unroll
@@ -126,69 +140,112 @@ chunk_fma_kernel(const __grid_constant__ ChunkParams p)
             for (int j = 0; j < 4; ++j) {
                 s[i][j] = chunk_ex2(s[i][j] - ref);
                 ps += s[i][j];
-                sm.p[tx * 4 + j][ty * RT + i] = s[i][j];
+                sm.p[ty + 16 * i][tx + 16 * j] = s[i][j];
             }
             m[i] = mn;
             sum[i] = sum[i] * corr + ps;   // this thread's share
 #pragma unroll
-            for (int c = 0; c < CV; ++c)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][c][e] *= corr;
+            for (int c = 0; c < CV; ++c) acc[i][c] = make_float4(acc[i][c].x * corr, acc[i][c].y * corr, acc[i][c].z * corr, acc[i][c].w * corr);
         }
-        __syncthreads();
-        const int here = min(kCfKeys, keys - k0);
-#pragma unroll 4
-        for (int j = 0; j < here; ++j) {
-            float a[RT];
-            if (RT == 4) *reinterpret_cast<float4 *>(a) = *reinterpret_cast<const float4 *>(&sm.p[j][ty * RT]);
-            else a[0] = sm.p[j][ty];
+        __syncwarp();   // a row of P is its half warp's own
+#pragma unroll 2
+        for (int j = 0; j < kCfKeys; j += 4) {   // (beyond the last key P and the values are zeros)
+            float4 a[4];
 #pragma unroll
-            for (int c = 0; c < CV; ++c) {
-                const float4 v4 = *reinterpret_cast<const float4 *>(&sm.v[j][c * 64 + tx * 4]);
-#pragma unroll
-                for (int i = 0; i < RT; ++i) {
-                    acc[i][c][0] = fmaf(a[i], v4.x, acc[i][c][0]);
-                    acc[i][c][1] = fmaf(a[i], v4.y, acc[i][c][1]);
-                    acc[i][c][2] = fmaf(a[i], v4.z, acc[i][c][2]);
-                    acc[i][c][3] = fmaf(a[i], v4.w, acc[i][c][3]);
-                }
-            }
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < RT; ++i) {
-#pragma unroll
-        for (int off = 8; off >= 1; off >>= 1) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], off);
-        const int r = ty * RT + i, t = (row0 + r) / G, g = row0 + r - t * G;
-        if (r >= rows) continue;
-        T *o = (T *)p.out + l * p.os.layer + b * p.os.stream + (long long)(hkv * G + g) * p.os.head + (long long)t * p.os.token;
-        const float inv = 1.f / sum[i];
-#pragma unroll
-        for (int c = 0; c < CV; ++c)
+            for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4 *>(&sm.p[ty + 16 * i][j]);
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (c * 64 + tx * 4 + e < p.d) o[c * 64 + tx * 4 + e] = from_float<T>(acc[i][c][e] * inv);
-        if (tx == 0 && p.lse) p.lse[(((size_t)l * p.streams + b) * p.Hkv * G + hkv * G + g) * p.n + t] = 0.6931471805599453f * (m[i] + log2f(sum[i]));
+#pragma unroll
+                for (int c = 0; c < CV; ++c) {
+                    const float4 v4 = *reinterpret_cast<const float4 *>(&sm.v[j + e][c * 64 + tx * 4]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float w = e == 0 ? a[i].x : e == 1 ? a[i].y : e == 2 ? a[i].z : a[i].w;
+                        const float2 lo = __ffma2_rn(make_float2(w, w), make_float2(v4.x, v4.y), make_float2(acc[i][c].x, acc[i][c].y));
+                        const float2 hi = __ffma2_rn(make_float2(w, w), make_float2(v4.z, v4.w), make_float2(acc[i][c].z, acc[i][c].w));
+                        acc[i][c] = make_float4(lo.x, lo.y, hi.x, hi.y);
+                    }
+                }
+        }
     }
+    const long long lse0 = ((long long)l * p.streams + b) * p.Hkv * G + hkv * G;
+    T *out = (T *)p.out + l * p.os.layer + b * p.os.stream + (long long)hkv * G * p.os.head;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int off = 8; off >= 1; off >>= 1) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], off);
+    }
+    if (ranks == 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = ty + 16 * i, t = (row0 + r) / G, g = row0 + r - t * G;
+            if (r >= rows) continue;
+            T *o = out + g * p.os.head + (long long)t * p.os.token;
+            const float inv = 1.f / sum[i];
+#pragma unroll
+            for (int c = 0; c < CV; ++c) {
+                struct alignas(4 * sizeof(T)) Four {
+                    T e[4];
+                } x;
+                x.e[0] = from_float<T>(acc[i][c].x * inv);
+                x.e[1] = from_float<T>(acc[i][c].y * inv);
+                x.e[2] = from_float<T>(acc[i][c].z * inv);
+                x.e[3] = from_float<T>(acc[i][c].w * inv);
+                if (c * 64 + tx * 4 < p.d) *reinterpret_cast<Four *>(o + c * 64 + tx * 4) = x;
+            }
+            if (tx == 0 && p.lse) p.lse[(lse0 + g) * p.n + t] = 0.6931471805599453f * (m[i] + log2f(sum[i]));
+        }
+        return;
+    }
+    // ---- the cluster: partial results in place of the keys, merged four channels of a row per thread
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = ty + 16 * i;
+#pragma unroll
+        for (int c = 0; c < CV; ++c) *reinterpret_cast<float4 *>(&sm.k[r][c * 64 + tx * 4]) = acc[i][c];
+        if (tx == 0) sm.stat[r] = make_float2(m[i], sum[i]);
+    }
+    cluster_sync();
+    for (int e = rank * kCfThreads + tid; e < rows * (p.d / 4); e += ranks * kCfThreads) {
+        const int r = e / (p.d / 4), c = e - r * (p.d / 4), t = (row0 + r) / G, g = row0 + r - t * G;
+        float ref = -INFINITY, den = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+        for (uint32_t k = 0; k < ranks; ++k) ref = fmaxf(ref, cluster_ld(cluster_addr(&sm.stat[r].x, k)));
+        for (uint32_t k = 0; k < ranks; ++k) {
+            const uint32_t st = cluster_addr(&sm.stat[r], k), src = cluster_addr(&sm.k[r][4 * c], k);
+            const float f = chunk_ex2(cluster_ld(st) - ref);   // (some rank has seen a key: ref is finite)
+            den = fmaf(cluster_ld(st + 4), f, den);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) o[x] = fmaf(cluster_ld(src + 4 * x), f, o[x]);
+        }
+        T *dst = out + g * p.os.head + (long long)t * p.os.token + 4 * c;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) dst[x] = from_float<T>(o[x] / den);
+        if (c == 0 && p.lse) p.lse[(lse0 + g) * p.n + t] = 0.6931471805599453f * (ref + log2f(den));
+    }
+    cluster_sync();   // no block ends while others read its results
 }
 
-template <typename T, int DP, int BM>
-inline cudaError_t launch_chunk_fma_t(const ChunkParams &p, cudaStream_t stream)
+template <typename T, int DP>
+inline cudaError_t launch_chunk_fma_t(const ChunkParams &p, int sm_count, cudaStream_t stream)
 {
-    const size_t smem = sizeof(ChunkFmaSmem<DP, BM>);
-    auto kern = chunk_fma_kernel<T, DP, BM>;
+    const size_t smem = sizeof(ChunkFmaSmem<DP>);
+    auto kern = chunk_fma_kernel<T, DP>;
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
     const int units = p.layers * p.streams * p.Hkv;
-    return launch_pdl(kern, dim3((unsigned)(((long long)p.n * p.G + BM - 1) / BM), units), dim3(kCfThreads), smem, stream, p);
+    const long long items = ((long long)p.n * p.G + kCfRows - 1) / kCfRows * units;
+    // blocks of a cluster: as many as SMs are left for, with two key tiles each
+    int cluster = 1;
+    while (cluster < 8 && items * cluster * 2 <= sm_count && p.len + p.n > 4 * cluster * kCfKeys) cluster *= 2;
+    if (items * cluster > 0x7fffffff) return cudaErrorInvalidValue;
+    return launch_cluster(kern, dim3((unsigned)(items * cluster)), dim3(kCfThreads), smem, cluster, stream, p, units);
 }
 
 template <typename T>
-inline cudaError_t launch_chunk_fma(const ChunkParams &p, cudaStream_t stream)
+inline cudaError_t launch_chunk_fma(const ChunkParams &p, int sm_count, cudaStream_t stream)
 {
-    if ((long long)p.n * p.G <= 16)
-        return p.d <= 64 ? launch_chunk_fma_t<T, 64, 16>(p, stream) : p.d <= 128 ? launch_chunk_fma_t<T, 128, 16>(p, stream) : launch_chunk_fma_t<T, 256, 16>(p, stream);
-    return p.d <= 64 ? launch_chunk_fma_t<T, 64, 64>(p, stream) : p.d <= 128 ? launch_chunk_fma_t<T, 128, 64>(p, stream) : launch_chunk_fma_t<T, 256, 64>(p, stream);
+    return p.d <= 64 ? launch_chunk_fma_t<T, 64>(p, sm_count, stream) : p.d <= 128 ? launch_chunk_fma_t<T, 128>(p, sm_count, stream) : launch_chunk_fma_t<T, 256>(p, sm_count, stream);
 }
 
 }  // namespace ipotk

@@ -17,8 +17,8 @@
 // raises the block's give-up flag and IPOT_E_TIMEOUT; from then on nothing more is put in flight, and what is in flight is
 // waited for before tensor memory is released.
 #pragma once
-#include "k_chunk_fma.cuh"
-#include "k_few.cuh"   // cluster_*
+#include "cluster.cuh"
+#include "k_chunk_fma.cuh"   // chunk_tokens, chunk_ex2
 #include "ops.h"
 #include "ptx.cuh"
 
@@ -517,20 +517,7 @@ inline cudaError_t launch_chunk_tc_t(const ChunkParams &c, const ChunkTcHost &ho
     p.withhold = host.withhold;
     p.wait_ns = host.wait_ns;
     p.status = c.status;
-    cudaLaunchConfig_t lc = {};
-    lc.gridDim = dim3((unsigned)cluster * p.items_per_unit * (unsigned)(c.layers * c.streams * c.Hkv));
-    lc.blockDim = dim3(L::kThreads);
-    lc.dynamicSmemBytes = L::kSmemBytes;
-    lc.stream = stream;
-    cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = cluster;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[1].val.programmaticStreamSerializationAllowed = 1;
-    lc.attrs = at;
-    lc.numAttrs = 2;
-    return cudaLaunchKernelEx(&lc, kern, q, K, V, k, v, p);
+    return launch_cluster(kern, dim3((unsigned)cluster * p.items_per_unit * (unsigned)(c.layers * c.streams * c.Hkv)), dim3(L::kThreads), L::kSmemBytes, cluster, stream, q, K, V, k, v, p);
 }
 
 inline cudaError_t launch_chunk_tc(const ChunkParams &c, const ChunkTcHost &host, cudaStream_t stream, bool *done)

@@ -18,43 +18,11 @@
 // Merge: the block's warps in shared memory, the cluster's blocks through distributed shared memory: no scratch, no atomics.
 #pragma once
 #include "common.cuh"
+#include "cluster.cuh"
 #include "ops.h"
 #include "k_rotary.cuh"   // RowVec, to_float, from_float
 
 namespace ipotk {
-
-// ------------------------------------------------------------------ the cluster
-__device__ __forceinline__ uint32_t cluster_rank()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t cluster_size()
-{
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync()
-{
-    __syncwarp();
-    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// The address of `p`, a pointer into this block's shared memory, in block `rank` of the cluster.
-__device__ __forceinline__ uint32_t cluster_addr(const void *p, uint32_t rank)
-{
-    uint32_t a;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
-    return a;
-}
-__device__ __forceinline__ float cluster_ld(uint32_t addr)
-{
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
-    return v;
-}
-__device__ __forceinline__ void cluster_st(uint32_t addr, double v) { asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(addr), "d"(v) : "memory"); }
 
 __device__ __forceinline__ float few_ex2(float x)
 {
@@ -738,23 +706,9 @@ few_fma_kernel(const __grid_constant__ FewParams p, int lpk)
 template <typename... A>
 inline cudaError_t launch_few_t(void (*kern)(FewParams, A...), const FewParams &p, size_t smem, int cluster, cudaStream_t stream, A... args)
 {
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e == cudaSuccess && cluster > 8) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    cudaLaunchConfig_t lc = {};
-    lc.gridDim = dim3(cluster, p.layers * p.streams * p.Hkv, (p.n * p.G + kFewRows - 1) / kFewRows);
-    lc.blockDim = dim3(kFewThreads);
-    lc.dynamicSmemBytes = smem;
-    lc.stream = stream;
-    cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeClusterDimension;
-    at[0].val.clusterDim.x = cluster;
-    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
-    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[1].val.programmaticStreamSerializationAllowed = 1;
-    lc.attrs = at;
-    lc.numAttrs = 2;
-    return cudaLaunchKernelEx(&lc, kern, p, args...);
+    return launch_cluster(kern, dim3(cluster, p.layers * p.streams * p.Hkv, (p.n * p.G + kFewRows - 1) / kFewRows), dim3(kFewThreads), smem, cluster, stream, p, args...);
 }
 
 template <int R, int VPL, bool kSparse>

@@ -41,7 +41,7 @@ cudaError_t launch_chunk_attention(const ChunkParams &p, bool f32, const ChunkTc
         f.scale_log2e = p.scale_log2e;
         return launch_few<false>(f, f32, host.sm_count, stream);
     }
-    if (f32) return launch_chunk_fma<float>(p, stream);
+    if (f32) return launch_chunk_fma<float>(p, host.sm_count, stream);
     if (host.encode && p.G <= kCtRows) {
         bool done = false;
         ChunkParams t = p;
@@ -49,7 +49,7 @@ cudaError_t launch_chunk_attention(const ChunkParams &p, bool f32, const ChunkTc
         const cudaError_t e = launch_chunk_tc(t, host, stream, &done);
         if (done || e != cudaSuccess) return e;
     }
-    return launch_chunk_fma<__nv_bfloat16>(p, stream);
+    return launch_chunk_fma<__nv_bfloat16>(p, host.sm_count, stream);
 }
 
 cudaError_t launch_block_bounds(const void *K, void *lo, void *hi, int first_row, int len, int rows, int d, int units, size_t unit_rows, int unit_blocks, bool f32,
