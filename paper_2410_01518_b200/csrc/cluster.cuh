@@ -21,6 +21,17 @@ __device__ __forceinline__ void cluster_sync()
     __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// The two halves of a barrier: what lies between them need not wait.
+__device__ __forceinline__ void cluster_arrive()
+{
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait()
+{
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 // The address of `p`, a pointer into this block's shared memory, in block `rank` of the cluster.
 __device__ __forceinline__ uint32_t cluster_addr(const void *p, uint32_t rank)
 {
@@ -34,6 +45,11 @@ __device__ __forceinline__ float cluster_ld(uint32_t addr)
     asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
     return v;
 }
+__device__ __forceinline__ void cluster_st(uint32_t addr, float4 v)
+{
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+__device__ __forceinline__ void cluster_st(uint32_t addr, float2 v) { asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(addr), "f"(v.x), "f"(v.y) : "memory"); }
 __device__ __forceinline__ void cluster_st(uint32_t addr, double v) { asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(addr), "d"(v) : "memory"); }
 
 // A launch of clusters along x (more than 8 blocks are not portable, but this part has 16), as a programmatic dependent like launch_pdl's.

@@ -8,14 +8,14 @@
 //   and lo where it is negative, so the heads' positive and negative parts are added first: s_b = sum_c (q+_c hi_bc + q-_c lo_bc), two
 //   products per channel whatever the number of heads.  In 64 bits: which block is in must not depend on the order of a sum.  The
 //   cluster's blocks share the scoring and put every score into each other's shared memory; then each finds, for itself, the
-//   (n - 1)-th largest of the order-preserving 64-bit keys bit by bit from the highest bit in which they differ (a count over the
-//   block per bit, and the search ends as soon as a count is right), and lists the chosen blocks in ascending order.
+//   (n - 1)-th largest of the order-preserving 64-bit keys by a search over its bits, and lists the chosen blocks in ascending order.
 // few_mma_kernel (bf16): a warp owns tiles of 16 keys and a ring of cp.async stages of its own, rows XOR-swizzled for ldmatrix;
 //   S^T = q K^T and O += P V are m16n8k16 tiles with fp32 accumulation.  Of the 16 rows 8 are queries: the other 8 of the output product hold the
 //   second of three bf16 terms of the weights where the result is fp32 (kSparse: 24 bits, nothing is rounded to bf16); a
 //   bf16 result takes the weights' first term.  tcgen05 does not fit: its smallest tile has 64 rows.
 // few_fma_kernel (f32): a group of lanes owns a key (a 16-byte vector of the row or two per lane), four keys at a time.
-// Merge: the block's warps in shared memory, the cluster's blocks through distributed shared memory: no scratch, no atomics.
+// Merge: the block's warps in shared memory; then every block of the cluster owns a share of the result and is sent what the others have of it
+// (stores into its shared memory: they are done by the time of the one barrier, which loads after it would not be).  No scratch, no atomics.
 #pragma once
 #include "common.cuh"
 #include "cluster.cuh"
@@ -33,7 +33,7 @@ __device__ __forceinline__ float few_ex2(float x)
 // 2^(m - ref), 0 where nothing has been seen (m = -inf) whatever ref is
 __device__ __forceinline__ float few_scale(float m, float ref) { return m == -INFINITY ? 0.f : few_ex2(m - ref); }
 
-constexpr int kFewThreads = 128, kFewWarps = kFewThreads / 32;
+constexpr int kFewThreads = 128, kFewWarps = kFewThreads / 32, kFewMaxRanks = 16;
 constexpr int kFewRows = 8;       // query rows of a block
 constexpr int kFewBlocks = 2048;  // blocks of a unit: 32768 slots, 16 rows
 
@@ -63,34 +63,162 @@ struct FewUnit {
     }
 };
 
-// ------------------------------------------------------------------ scores and selection
-struct BlockSelection {
-    uint16_t list[kFewBlocks];
-    unsigned long long reach[2][kFewWarps];
-    int count[2][kFewWarps];
+// Shared memory besides the keys' ring.
+struct FewShared {
+    uint16_t list[kFewBlocks];                     // the chosen blocks
+    uint2 reach[kFewWarps];
+    unsigned long long count[2][kFewWarps];
+    float2 warp_stat[kFewWarps][kFewRows];      // (reference in binary orders, sum) of the warps,
+    float weight[kFewWarps][kFewRows];          // what their results are multiplied by,
+    float2 stat[kFewMaxRanks][kFewRows];           // and of the cluster's blocks
 };
 
-// Monotone map double -> uint64.
+// ------------------------------------------------------------------ scores and selection
+// Monotone map double -> uint64; no finite number becomes 0.
 __device__ __forceinline__ unsigned long long order_key64(double s)
 {
     const unsigned long long b = (unsigned long long)__double_as_longlong(s + 0.0);   // (-0 counts as 0)
     return b ^ ((unsigned long long)((long long)b >> 63) | 0x8000000000000000ull);
 }
 
-// All blocks of the cluster: sel.list becomes the ascending list of the chosen blocks, its length is returned.  score: kFewBlocks numbers of
-// shared memory that is free meanwhile, at the same place in every block.
-template <typename T>
-__device__ __forceinline__ int select_blocks(BlockSelection &sel, double *score, const FewParams &p, const FewUnit &u)
+// The ascending list of the `need` largest of `others` keys (ties: the lower block); a thread has up to KPT neighbouring blocks.  The keys are taken apart at
+// the highest bit in which they differ: 32 bits from there decide nearly always, those below them where that leaves a tie.  Two bits a step: three counts
+// in one sum over the warp, one barrier a step, and the search ends as soon as a count is right.  (One warp with 8 keys a lane and no barrier: 600 cycles
+// a step, this 130.)
+template <int KPT>
+__device__ __forceinline__ void select_in_block(FewShared &sh, const double *score, int others, int need)
 {
-    constexpr int VE = RowVec<T>::kElems, NV = sizeof(T) == 2 ? 2 : 4, KPT = kFewBlocks / kFewThreads;   // 256 channels: 64 vectors of bf16 bounds, 128 of f32
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, vecs = p.d / VE, pieces = 2 * vecs;
-    const int total = (p.len + p.block_rows - 1) / p.block_rows, want = min(p.blocks, total);
-    if (want == total) {
-        for (int b = threadIdx.x; b < total; b += kFewThreads) sel.list[b] = b;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per = (others + kFewThreads - 1) / kFewThreads, first = threadIdx.x * per, here = max(0, min(per, others - first));
+    uint32_t hi[KPT], lo[KPT];   // 0 where there is no block
+    {
+        unsigned long long key[KPT];
+        uint32_t top = 0, low = 0xffffffffu;
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) {
+            key[i] = 0;
+            if (i < here) {
+                key[i] = order_key64(score[first + i]);
+                top = max(top, (uint32_t)(key[i] >> 32));
+                low = min(low, (uint32_t)(key[i] >> 32));
+            }
+        }
+        top = __reduce_max_sync(0xffffffffu, top);
+        low = __reduce_min_sync(0xffffffffu, low);
+        if (lane == 0) sh.reach[warp] = make_uint2(top, low);
         __syncthreads();
+#pragma unroll
+        for (int v = 0; v < kFewWarps; ++v) {
+            top = max(top, sh.reach[v].x);
+            low = min(low, sh.reach[v].y);
+        }
+        // (where the upper halves agree the whole lower ones are compared)
+        const int shift = top != low ? 32 - __clz(top ^ low) : 0;   // bits below the 32 that are looked at first
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) {
+            hi[i] = (uint32_t)(key[i] >> shift);
+            lo[i] = shift ? (uint32_t)(key[i] << (32 - shift)) : 0u;
+        }
+    }
+    int parity = 0;
+    // the block's sum of three counts, 21 bits each
+    auto block_sum = [&](uint32_t c) {   // (ten bits each: at most 512 in a warp)
+        c = __reduce_add_sync(0xffffffffu, c);
+        if (lane == 0) sh.count[parity][warp] = (c & 1023) | (unsigned long long)(c >> 10 & 1023) << 21 | (unsigned long long)(c >> 20) << 42;
+        __syncthreads();
+        unsigned long long all = 0;
+#pragma unroll
+        for (int v = 0; v < kFewWarps; ++v) all += sh.count[parity][v];
+        parity ^= 1;
+        return all;
+    };
+    uint32_t in = 0, group = here > 0 ? 0xffffffffu >> (32 - here) : 0u;   // bit i: block first + i is in; may still be
+    int left = need;
+#pragma unroll 1
+    for (int level = 0; level < 2 && left > 0; ++level) {
+        uint32_t k[KPT], at = 0;
+#pragma unroll
+        for (int i = 0; i < KPT; ++i) k[i] = group >> i & 1 ? (level ? lo[i] : hi[i]) : 0u;   // (`at` with a bit set is never 0)
+        bool exact = false;
+#pragma unroll 1
+        for (int bit = 30; bit >= 0 && !exact; bit -= 2) {
+            uint32_t c1 = 0, c2 = 0, c3 = 0;
+#pragma unroll
+            for (int i = 0; i < KPT; ++i) {
+                c1 += k[i] >= (at | 1u << bit);
+                c2 += k[i] >= (at | 2u << bit);
+                c3 += k[i] >= (at | 3u << bit);
+            }
+            const unsigned long long all = block_sum(c1 | c2 << 10 | c3 << 20);
+            const int n1 = (int)(all & 0x1fffff), n2 = (int)(all >> 21 & 0x1fffff), n3 = (int)(all >> 42);
+            at |= (n3 >= left ? 3u : n2 >= left ? 2u : n1 >= left ? 1u : 0u) << bit;
+            exact = n1 == left || n2 == left || n3 == left;
+        }
+        uint32_t above = 0, equal = 0;
+#pragma unroll
+        for (int i = 0; i < KPT; ++i)
+            if (group >> i & 1) {
+                above |= (uint32_t)(k[i] > at || (exact && k[i] == at)) << i;
+                equal |= (uint32_t)(!exact && k[i] == at) << i;
+            }
+        in |= above;
+        group = equal;
+        left = exact ? 0 : left - (int)(block_sum(__popc(above)) & 0x1fffff);
+    }
+    // `left` of those that agree in all bits, the lower blocks, are in too.  Places by an exclusive sum over the threads, both counts in one number
+    const int both = __popc(in) | __popc(group) << 16;
+    int incl = both;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, incl, off);
+        if (lane >= off) incl += v;
+    }
+    if (lane == 31) sh.count[parity][warp] = (unsigned)incl;
+    __syncthreads();
+    int before = incl - both;
+#pragma unroll
+    for (int v = 0; v < kFewWarps; ++v)
+        if (v < warp) before += (int)sh.count[parity][v];
+    int equal_before = before >> 16, place = (before & 0xffff) + min(equal_before, left);
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) {
+        bool is = in >> i & 1;
+        if (group >> i & 1) is = equal_before++ < left;
+        if (is) sh.list[place++] = (uint16_t)(first + i);
+    }
+}
+
+// All blocks of the cluster: sh.list becomes the ascending list of the chosen blocks, its length is returned.  score: kFewBlocks numbers of
+// shared memory that is free meanwhile, at the same place in every block.  The cluster has arrived at its first barrier.
+template <typename T>
+__device__ __forceinline__ int select_blocks(FewShared &sh, double *score, const FewParams &p, const FewUnit &u)
+{
+    constexpr int VE = RowVec<T>::kElems, NV = sizeof(T) == 2 ? 2 : 4;   // 256 channels: 64 vectors of bf16 bounds, 128 of f32
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, vecs = p.d / VE, pieces = 2 * vecs;
+    const int total = (p.len + p.block_rows - 1) / p.block_rows, want = min(p.blocks, total), others = total - 1, need = want - 1;
+    if (want == total || need == 0) {
+        for (int b = threadIdx.x; b < want; b += kFewThreads) sh.list[b] = (uint16_t)(need == 0 ? others : b);
+        __syncthreads();
+        cluster_wait();
         return want;
     }
-    // this lane's channels: vector lane + 32 i of a block's lower, then upper bounds; what the heads' queries sum up to there
+    // this lane's channels: vector lane + 32 i of a block's lower, then upper bounds
+    const T *lo = (const T *)p.lo + (size_t)u.unit * p.unit_blocks * p.d, *hi = (const T *)p.hi + (size_t)u.unit * p.unit_blocks * p.d;
+    constexpr int BF = 4;   // blocks whose bounds are on their way at once
+    const int stride = u.ranks * kFewWarps;
+    RowVec<T> x[BF][NV], x_next[BF][NV];
+    auto fetch = [&](RowVec<T> (&x)[BF][NV], int b0) {
+#pragma unroll
+        for (int f = 0; f < BF; ++f)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int piece = lane + 32 * i, b = min(b0 + f * stride, others - 1);
+                const bool upper = piece >= vecs;
+                if (piece < pieces) x[f][i] = *reinterpret_cast<const RowVec<T> *>((upper ? hi : lo) + (size_t)b * p.d + (piece - (upper ? vecs : 0)) * VE);
+            }
+    };
+    int b0 = u.rank * kFewWarps + warp;
+    fetch(x, b0);
+    // what the heads' queries sum up to in those channels, above and below zero
     double w[NV * VE];
     const T *q = (const T *)p.q + u.l * p.qs.layer + u.b * p.qs.stream + (long long)u.hkv * p.G * p.qs.head;
 #pragma unroll
@@ -100,198 +228,129 @@ __device__ __forceinline__ int select_blocks(BlockSelection &sel, double *score,
         for (int e = 0; e < VE; ++e) w[i * VE + e] = 0.0;
         if (piece >= pieces) continue;
         const bool upper = piece >= vecs;
-        for (int h = 0; h < p.G; ++h) {
-            const RowVec<T> x = *reinterpret_cast<const RowVec<T> *>(q + h * p.qs.head + (piece - (upper ? vecs : 0)) * VE);
+        constexpr int HB = 8;   // heads on their way at once
+#pragma unroll 1
+        for (int h0 = 0; h0 < p.G; h0 += HB) {
+            RowVec<T> y[HB];
 #pragma unroll
-            for (int e = 0; e < VE; ++e) {
-                const float f = to_float(x.e[e]);
-                if (upper ? f > 0.f : f < 0.f) w[i * VE + e] += (double)f;
-            }
+            for (int h = 0; h < HB; ++h) y[h] = *reinterpret_cast<const RowVec<T> *>(q + min(h0 + h, p.G - 1) * p.qs.head + (piece - (upper ? vecs : 0)) * VE);
+#pragma unroll
+            for (int h = 0; h < HB; ++h)
+#pragma unroll
+                for (int e = 0; e < VE; ++e) {
+                    const float f = to_float(y[h].e[e]);
+                    w[i * VE + e] += (double)(h0 + h < p.G ? (upper ? fmaxf(f, 0.f) : fminf(f, 0.f)) : 0.f);
+                }
         }
     }
-    const T *lo = (const T *)p.lo + (size_t)u.unit * p.unit_blocks * p.d, *hi = (const T *)p.hi + (size_t)u.unit * p.unit_blocks * p.d;
-    constexpr int BF = 4;   // blocks whose bounds are on their way at once
-    const int stride = u.ranks * kFewWarps;
-    for (int b0 = u.rank * kFewWarps + warp; b0 < total - 1; b0 += BF * stride) {
-        RowVec<T> x[BF][NV];
+    cluster_wait();   // all of the cluster has started: its shared memory may be written
+    for (;;) {
+        const bool more = b0 + BF * stride < others;
+        if (more) fetch(x_next, b0 + BF * stride);
+        double sum[BF];   // of four blocks side by side: the chains of 64-bit sums are long
+#pragma unroll
+        for (int f = 0; f < BF; ++f) sum[f] = 0.0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            if (lane + 32 * i < pieces) {
+#pragma unroll
+                for (int e = 0; e < VE; ++e)
+#pragma unroll
+                    for (int f = 0; f < BF; ++f) sum[f] = fma(w[i * VE + e], (double)to_float(x[f][i].e[e]), sum[f]);
+            }
+        // sums over the lanes: a lane keeps half of what it has and sends the other half, so that lanes 8 f .. 8 f + 7 end with block f's
+        static_assert(BF == 4, "two halvings");
+        {
+            const bool up = lane & 16;
+            const double s0 = __shfl_xor_sync(0xffffffffu, up ? sum[0] : sum[2], 16), s1 = __shfl_xor_sync(0xffffffffu, up ? sum[1] : sum[3], 16);
+            sum[0] = (up ? sum[2] : sum[0]) + s0;
+            sum[1] = (up ? sum[3] : sum[1]) + s1;
+        }
+        {
+            const bool up = lane & 8;
+            const double s0 = __shfl_xor_sync(0xffffffffu, up ? sum[0] : sum[1], 8);
+            sum[0] = (up ? sum[1] : sum[0]) + s0;
+        }
+#pragma unroll
+        for (int off = 4; off >= 1; off >>= 1) sum[0] += __shfl_xor_sync(0xffffffffu, sum[0], off);
+        const int b = b0 + (lane >> 3) * stride;
+        if (b < others)
+            for (uint32_t r = lane & 7; r < u.ranks; r += 8) cluster_st(cluster_addr(score + b, r), sum[0]);
+        if (!more) break;
+        b0 += BF * stride;
 #pragma unroll
         for (int f = 0; f < BF; ++f)
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int piece = lane + 32 * i, b = b0 + f * stride;
-                const bool upper = piece >= vecs;
-                if (piece < pieces && b < total - 1) x[f][i] = *reinterpret_cast<const RowVec<T> *>((upper ? hi : lo) + (size_t)b * p.d + (piece - (upper ? vecs : 0)) * VE);
-            }
-#pragma unroll
-        for (int f = 0; f < BF; ++f) {
-            const int b = b0 + f * stride;
-            if (b >= total - 1) break;
-            double s = 0.0;
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-                if (lane + 32 * i < pieces) {
-#pragma unroll
-                    for (int e = 0; e < VE; ++e) s = fma(w[i * VE + e], (double)to_float(x[f][i].e[e]), s);
-                }
-#pragma unroll
-            for (int off = 16; off >= 1; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-            if (lane < (int)u.ranks) cluster_st(cluster_addr(score + b, lane), s);
-        }
+            for (int i = 0; i < NV; ++i) x[f][i] = x_next[f][i];
     }
     cluster_sync();
-    // a thread has the keys of `per` neighbouring blocks; the newest block is in and stands outside
-    const int others = total - 1, per = (others + kFewThreads - 1) / kFewThreads, first = threadIdx.x * per, here = max(0, min(per, others - first));
-    unsigned long long key[KPT], top = 0, low = ~0ull;
-#pragma unroll
-    for (int i = 0; i < KPT; ++i) {
-        key[i] = 0;
-        if (i < here) {
-            key[i] = order_key64(score[first + i]);
-            top = max(top, key[i]);
-            low = min(low, key[i]);
-        }
-    }
-#pragma unroll
-    for (int off = 16; off >= 1; off >>= 1) {
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
-        low = min(low, __shfl_xor_sync(0xffffffffu, low, off));
-    }
-    if (lane == 0) {
-        sel.reach[0][warp] = top;
-        sel.reach[1][warp] = low;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int w2 = 0; w2 < kFewWarps; ++w2) {
-        top = max(top, sel.reach[0][w2]);
-        low = min(low, sel.reach[1][w2]);
-    }
-    const int need = want - 1;
-    auto block_sum = [&](int v, int parity) {
-        v = __reduce_add_sync(0xffffffffu, v);
-        if (lane == 0) sel.count[parity][warp] = v;
-        __syncthreads();
-        int s = 0;
-#pragma unroll
-        for (int w2 = 0; w2 < kFewWarps; ++w2) s += sel.count[parity][w2];
-        return s;
-    };
-    // the largest `at` such that at least `need` keys are >= at (all bits of the common prefix are those of every key)
-    unsigned long long at = 0;
-    bool exact = false;   // exactly the keys >= at are in
-    int parity = 0;
-    if (need > 0) {
-        const unsigned long long diff = top ^ low;
-        int bit = diff ? 63 - __clzll((long long)diff) : -1;
-        at = bit >= 0 ? top & ~((2ull << bit) - 1) : top;
-        for (; bit >= 0 && !exact; --bit) {
-            const unsigned long long cand = at | (1ull << bit);
-            int c = 0;
-#pragma unroll
-            for (int i = 0; i < KPT; ++i) {
-                if (i >= per) break;
-                c += i < here && key[i] >= cand;
-            }
-            c = block_sum(c, parity);
-            parity ^= 1;
-            if (c >= need) at = cand;
-            exact = c == need;
-        }
-    }
-    // keys above `at` are in, and of those equal to it the first ones (all of them where the count was exact)
-    int above = 0, equal = 0;
-#pragma unroll
-    for (int i = 0; i < KPT; ++i) {
-        above += i < here && key[i] > at;
-        equal += i < here && key[i] == at;
-    }
-    if (need == 0) above = equal = 0;
-    // exclusive sums over the threads before this one: both counts in one number
-    int both = above | equal << 16, incl = both;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-        const int v = __shfl_up_sync(0xffffffffu, incl, off);
-        if (lane >= off) incl += v;
-    }
-    if (lane == 31) sel.count[parity][warp] = incl;
-    __syncthreads();
-    int before = incl - both, all = 0;
-#pragma unroll
-    for (int w2 = 0; w2 < kFewWarps; ++w2) {
-        const int c = sel.count[parity][w2];
-        if (w2 < warp) before += c;
-        all += c;
-    }
-    const int take_equal = need - (all & 0xffff);
-    int eq_before = before >> 16, place = (before & 0xffff) + min(eq_before, take_equal);
-    if (need > 0) {
-#pragma unroll
-        for (int i = 0; i < KPT; ++i) {
-            if (i >= here) continue;
-            bool in = key[i] > at;
-            if (key[i] == at) in = eq_before++ < take_equal;
-            if (in) sel.list[place++] = first + i;
-        }
-    }
-    if (threadIdx.x == 0) sel.list[need] = total - 1;
+    if (others <= 2 * kFewThreads) select_in_block<2>(sh, score, others, need);
+    else select_in_block<kFewBlocks / kFewThreads>(sh, score, others, need);
+    if (threadIdx.x == 0) sh.list[need] = (uint16_t)others;
     __syncthreads();
     return want;
 }
 
 // ------------------------------------------------------------------ the end of a block's work
-// part: [warps][rows][d + 2] (output against a reference, the reference in binary orders, the sum); mine: [rows][d + 2] of this block.
+// part: [warps][rows][d + 4] outputs against the references in sh.warp_stat; got: room for the blocks' shares of the result.
 template <typename O>
-__device__ __forceinline__ void few_finish(float *part, float *mine, const FewParams &p, const FewUnit &u)
+__device__ __forceinline__ void few_finish(float *part, float *got, FewShared &sh, const FewParams &p, const FewUnit &u)
 {
-    const int ds = p.d + 2;
+    const int ds = p.d + 4, all = u.rows * p.d, share = ((all + (int)u.ranks - 1) / (int)u.ranks + 3) & ~3;
     __syncthreads();
-    for (int e = threadIdx.x; e < u.rows * ds; e += kFewThreads) {
-        const int h = e / ds, c = e - h * ds;
-        float ref = -INFINITY;
+    for (int e = threadIdx.x; e < u.rows * (int)u.ranks; e += kFewThreads) {   // a row's statistics to one block of the cluster
+        const int r = e / u.rows, h = e - r * u.rows;
+        float ref = -INFINITY, sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < kFewWarps; ++w) ref = fmaxf(ref, part[(w * u.rows + h) * ds + p.d]);
-        float v = ref;
-        if (c != p.d) {
-            v = 0.f;
+        for (int w = 0; w < kFewWarps; ++w) ref = fmaxf(ref, sh.warp_stat[w][h].x);
 #pragma unroll
-            for (int w = 0; w < kFewWarps; ++w) v = fmaf(part[(w * u.rows + h) * ds + c], few_scale(part[(w * u.rows + h) * ds + p.d], ref), v);
+        for (int w = 0; w < kFewWarps; ++w) {
+            const float f = few_scale(sh.warp_stat[w][h].x, ref);
+            sum = fmaf(sh.warp_stat[w][h].y, f, sum);
+            if (r == 0) sh.weight[w][h] = f;
         }
-        mine[e] = v;
+        cluster_st(cluster_addr(&sh.stat[u.rank][h], r), make_float2(ref, sum));
     }
-    cluster_sync();
-    for (int e = u.rank * kFewThreads + threadIdx.x; e < u.rows * p.d; e += u.ranks * kFewThreads) {
+    __syncthreads();
+    for (int e = threadIdx.x * 4; e < all; e += kFewThreads * 4) {
+        const int h = e / p.d, c = e - h * p.d, owner = e / share;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < kFewWarps; ++w) {
+            const float4 x = *reinterpret_cast<const float4 *>(part + (w * u.rows + h) * ds + c);
+            const float f = sh.weight[w][h];
+            v = make_float4(fmaf(x.x, f, v.x), fmaf(x.y, f, v.y), fmaf(x.z, f, v.z), fmaf(x.w, f, v.w));
+        }
+        cluster_st(cluster_addr(got + u.rank * share + e - owner * share, owner), v);
+    }
+    cluster_sync();   // from here on a block touches its own memory alone
+    for (int i = threadIdx.x; i < share; i += kFewThreads) {
+        const int e = u.rank * share + i;
+        if (e >= all) break;
         const int h = e / p.d, c = e - h * p.d;
-        float ref = -INFINITY, o = 0.f, den = 0.f;
-        constexpr int RB = 4;   // ranks whose values are on their way at once
-        for (uint32_t r0 = 0; r0 < u.ranks; r0 += RB) {
-            float m[RB], s[RB], x[RB];
+        float ref = -INFINITY, o = 0.f, sum = 0.f;
+        float2 st[kFewMaxRanks];
+        float x[kFewMaxRanks];
 #pragma unroll
-            for (int i = 0; i < RB; ++i) {
-                const uint32_t r = min(r0 + i, u.ranks - 1);
-                m[i] = cluster_ld(cluster_addr(mine + h * ds + p.d, r));
-                s[i] = cluster_ld(cluster_addr(mine + h * ds + p.d + 1, r));
-                x[i] = cluster_ld(cluster_addr(mine + h * ds + c, r));
-                if (r0 + i >= u.ranks) m[i] = -INFINITY;
+        for (uint32_t r = 0; r < kFewMaxRanks; ++r) {
+            st[r] = make_float2(-INFINITY, 0.f);
+            x[r] = 0.f;
+            if (r < u.ranks) {
+                st[r] = sh.stat[r][h];
+                x[r] = got[r * share + i];
             }
-            float top = ref;
+            ref = fmaxf(ref, st[r].x);
+        }
 #pragma unroll
-            for (int i = 0; i < RB; ++i) top = fmaxf(top, m[i]);
-            const float f0 = few_scale(ref, top);
-            o *= f0;
-            den *= f0;
-            ref = top;
-#pragma unroll
-            for (int i = 0; i < RB; ++i) {
-                const float f = few_scale(m[i], ref);
-                o = fmaf(x[i], f, o);
-                den = fmaf(s[i], f, den);
-            }
+        for (uint32_t r = 0; r < kFewMaxRanks; ++r) {
+            const float f = few_scale(st[r].x, ref);
+            o = fmaf(x[r], f, o);
+            sum = fmaf(st[r].y, f, sum);
         }
         const int t = (u.row0 + h) / p.G, g = u.hkv * p.G + u.row0 + h - t * p.G;
-        ((O *)p.out)[u.l * p.os.layer + u.b * p.os.stream + g * p.os.head + (long long)t * p.os.token + c] = from_float<O>(o / den);
-        if (c == 0 && p.lse) p.lse[(((size_t)u.l * p.streams + u.b) * p.Hkv * p.G + g) * p.n + t] = 0.6931471805599453f * (ref + log2f(den));
+        ((O *)p.out)[u.l * p.os.layer + u.b * p.os.stream + g * p.os.head + (long long)t * p.os.token + c] = from_float<O>(o / sum);
+        if (c == 0 && p.lse) p.lse[(((size_t)u.l * p.streams + u.b) * p.Hkv * p.G + g) * p.n + t] = 0.6931471805599453f * (ref + log2f(sum));
     }
-    cluster_sync();   // no block ends while others read its results
 }
 
 // Tiles of 16 keys: kSparse, of the selected blocks; else of the pot's rows and, the last one, of the chunk's.
@@ -325,7 +384,8 @@ template <bool kSparse> struct FewTiles {
 constexpr int kFewStages = 3;
 template <int D> struct FewRing {
     static constexpr size_t kBytes = (size_t)kFewWarps * kFewStages * 2 * 16 * D * 2;
-    static_assert(kBytes >= kFewBlocks * sizeof(double) && kBytes >= (kFewWarps + 1) * kFewRows * (D + 2) * 4, "scores and the merge take its place");
+    static constexpr size_t kGot = (kFewRows * D + 4 * kFewMaxRanks) * sizeof(float);
+    static_assert(kBytes >= kFewBlocks * sizeof(double) && kBytes >= kFewWarps * kFewRows * (D + 4) * sizeof(float), "scores and the merge take its place");
 };
 
 __device__ __forceinline__ void few_cp_async16(void *dst, const void *src, bool there)
@@ -358,56 +418,20 @@ template <int D, bool kSparse>
 __global__ void __launch_bounds__(kFewThreads)
 few_mma_kernel(const __grid_constant__ FewParams p)
 {
+    cluster_arrive();
     pdl_wait();
     pdl_release();
     using T = __nv_bfloat16;
     constexpr int VPR = D / 8, NT = D / 8, STAGE = 16 * VPR;   // 16-byte vectors of a row, output tiles of 8 channels, vectors of a stage's keys
     extern __shared__ __align__(16) uint8_t few_raw[];
     const FewUnit u(p);
-    BlockSelection *sel = reinterpret_cast<BlockSelection *>(few_raw + FewRing<D>::kBytes);
-    int selected = 0;
-    if (kSparse) {
-        cluster_sync();   // all of the cluster has started: its shared memory may be written
-        selected = select_blocks<T>(*sel, reinterpret_cast<double *>(few_raw), p, u);
-        if (p.list && u.rank == 0 && u.row0 == 0)
-            for (int i = threadIdx.x; i < p.blocks; i += kFewThreads) p.list[(size_t)blockIdx.y * p.blocks + i] = i < selected ? sel->list[i] : -1;
-    } else if (u.rows <= 0) {
-        return;   // (the whole cluster)
-    }
-    const FewTiles<kSparse> tiles(p, u, selected);
+    using Ring = FewRing<D>;
+    FewShared &sh = *reinterpret_cast<FewShared *>(few_raw + Ring::kBytes);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = lane >> 2, tq = lane & 3, vecs = p.d / 8;
-    const uint4 *K = reinterpret_cast<const uint4 *>((const T *)p.K + (size_t)u.unit * p.unit_rows * p.d);
-    const uint4 *V = reinterpret_cast<const uint4 *>((const T *)p.V + (size_t)u.unit * p.unit_rows * p.d);
-    uint4 *ring = reinterpret_cast<uint4 *>(few_raw) + (size_t)warp * kFewStages * 2 * STAGE;
-    const int w0 = u.rank * kFewWarps + warp, step = u.ranks * kFewWarps, mine = tiles.all > w0 ? (tiles.all - w0 + step - 1) / step : 0;
-
-    auto issue = [&](int i) {   // this warp's i-th tile into stage i % kFewStages
-        if (i < mine) {
-            int row, count;
-            bool fresh;
-            tiles.locate(p, u, kSparse ? sel->list : nullptr, w0 + i * step, row, count, fresh);
-            const uint4 *gk = K + (size_t)row * vecs, *gv = V + (size_t)row * vecs;
-            long long pk = vecs, pv = vecs;   // of a row
-            if (!kSparse && fresh) {
-                gk = reinterpret_cast<const uint4 *>((const T *)p.k + u.l * p.ks.layer + u.b * p.ks.stream + u.hkv * p.ks.head);
-                gv = reinterpret_cast<const uint4 *>((const T *)p.v + u.l * p.vs.layer + u.b * p.vs.stream + u.hkv * p.vs.head);
-                pk = p.ks.token / 8;
-                pv = p.vs.token / 8;
-            }
-            uint4 *sk = ring + (size_t)(i % kFewStages) * 2 * STAGE, *sv = sk + STAGE;
-#pragma unroll
-            for (int x = 0; x < STAGE / 32; ++x) {
-                const int e = x * 32 + lane, r = e / VPR, c = e - r * VPR, at = r * VPR + (c ^ (r & 7));
-                const bool there = r < count && c < vecs;   // what is not becomes zeros
-                few_cp_async16(sk + at, there ? gk + r * pk + c : K, there);
-                few_cp_async16(sv + at, there ? gv + r * pv + c : V, there);
-            }
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-#pragma unroll
-    for (int i = 0; i < kFewStages - 1; ++i) issue(i);
-
+    if (!kSparse && u.rows <= 0) {   // (the whole cluster)
+        cluster_wait();
+        return;
+    }
     // A fragments of the queries: row quad, rows 8 .. 15 are zero
     uint32_t qa[D / 16][2];
     {
@@ -420,6 +444,46 @@ few_mma_kernel(const __grid_constant__ FewParams p)
                 qa[ks][x] = quad < u.rows && c < p.d ? __ldg(reinterpret_cast<const uint32_t *>(qr + c)) : 0u;
             }
     }
+    const int selected = kSparse ? select_blocks<T>(sh, reinterpret_cast<double *>(few_raw), p, u) : 0;
+    const FewTiles<kSparse> tiles(p, u, selected);
+    const uint4 *K = reinterpret_cast<const uint4 *>((const T *)p.K + (size_t)u.unit * p.unit_rows * p.d);
+    const uint4 *V = reinterpret_cast<const uint4 *>((const T *)p.V + (size_t)u.unit * p.unit_rows * p.d);
+    uint4 *ring = reinterpret_cast<uint4 *>(few_raw) + (size_t)warp * kFewStages * 2 * STAGE;
+    const int w0 = u.rank * kFewWarps + warp, step = u.ranks * kFewWarps, mine = tiles.all > w0 ? (tiles.all - w0 + step - 1) / step : 0;
+
+    auto issue = [&](int i) {   // this warp's i-th tile into stage i % kFewStages
+        if (i < mine) {
+            int row, count;
+            bool fresh;
+            tiles.locate(p, u, sh.list, w0 + i * step, row, count, fresh);
+            constexpr int RX = 32 / VPR;   // rows that the warp's lanes cover
+            const int r0 = lane / VPR, c = lane - r0 * VPR;
+            const uint4 *gk = K + (size_t)row * vecs, *gv = V + (size_t)row * vecs;
+            long long pk = vecs, pv = vecs;   // of a row
+            if (!kSparse && fresh) {
+                gk = reinterpret_cast<const uint4 *>((const T *)p.k + u.l * p.ks.layer + u.b * p.ks.stream + u.hkv * p.ks.head);
+                gv = reinterpret_cast<const uint4 *>((const T *)p.v + u.l * p.vs.layer + u.b * p.vs.stream + u.hkv * p.vs.head);
+                pk = p.ks.token / 8;
+                pv = p.vs.token / 8;
+            }
+            gk += r0 * pk + c;
+            gv += r0 * pv + c;
+            uint4 *sk = ring + (size_t)(i % kFewStages) * 2 * STAGE, *sv = sk + STAGE;
+#pragma unroll
+            for (int x = 0; x < 16 / RX; ++x, gk += RX * pk, gv += RX * pv) {
+                const int r = x * RX + r0, at = r * VPR + (c ^ (r & 7));
+                const bool there = r < count && c < vecs;   // what is not becomes zeros
+                few_cp_async16(sk + at, there ? gk : K, there);
+                few_cp_async16(sv + at, there ? gv : V, there);
+            }
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int i = 0; i < kFewStages - 1; ++i) issue(i);
+
+    if (kSparse && p.list && u.rank == 0 && u.row0 == 0)
+        for (int i = threadIdx.x; i < p.blocks; i += kFewThreads) p.list[(size_t)blockIdx.y * p.blocks + i] = i < selected ? sh.list[i] : -1;
     const int seen = (u.row0 + quad) / p.G + 1;   // of the chunk's rows
     float o[NT][4];
 #pragma unroll
@@ -432,22 +496,26 @@ few_mma_kernel(const __grid_constant__ FewParams p)
         issue(i + kFewStages - 1);
         int row, count;
         bool fresh;
-        tiles.locate(p, u, kSparse ? sel->list : nullptr, w0 + i * step, row, count, fresh);
+        tiles.locate(p, u, sh.list, w0 + i * step, row, count, fresh);
         if (count <= 0) continue;
         if (!kSparse && fresh) count = min(count, seen);
         const uint32_t sk = (uint32_t)__cvta_generic_to_shared(ring + (size_t)(i % kFewStages) * 2 * STAGE), sv = sk + STAGE * 16;
         // ---- S^T = q K^T for 16 keys: two column tiles of 8
-        float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
+        float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f}, z0[4] = {0.f, 0.f, 0.f, 0.f}, z1[4] = {0.f, 0.f, 0.f, 0.f};   // (even and odd steps: shorter chains)
         {
             const int r = (lane & 7) + ((lane >> 4) & 1) * 8, cs = (lane >> 3) & 1;
 #pragma unroll
             for (int ks = 0; ks < D / 16; ++ks) {
                 uint32_t b[4];
                 few_ldmatrix(b, sk + (uint32_t)(r * VPR + ((2 * ks + cs) ^ (r & 7))) * 16);
-                few_mma(s0, qa[ks][0], 0u, qa[ks][1], 0u, b[0], b[1]);
-                few_mma(s1, qa[ks][0], 0u, qa[ks][1], 0u, b[2], b[3]);
+                few_mma(ks & 1 ? z0 : s0, qa[ks][0], 0u, qa[ks][1], 0u, b[0], b[1]);
+                few_mma(ks & 1 ? z1 : s1, qa[ks][0], 0u, qa[ks][1], 0u, b[2], b[3]);
             }
         }
+        s0[0] += z0[0];
+        s0[1] += z0[1];
+        s1[0] += z1[0];
+        s1[1] += z1[1];
         // this lane: row quad, keys 2 tq, + 1 and 8 + 2 tq, + 1 of the tile; the first key is there for every row
         float sc[4] = {s0[0] * p.scale_log2e, s0[1] * p.scale_log2e, s1[0] * p.scale_log2e, s1[1] * p.scale_log2e}, mt = -INFINITY;
 #pragma unroll
@@ -512,23 +580,17 @@ few_mma_kernel(const __grid_constant__ FewParams p)
     l += __shfl_xor_sync(0xffffffffu, l, 1);
     l += __shfl_xor_sync(0xffffffffu, l, 2);
     __syncthreads();   // every warp has left its ring: the memory now carries the merge
-    float *part = reinterpret_cast<float *>(few_raw);
-    const int ds = p.d + 2;
+    float *part = reinterpret_cast<float *>(few_raw), *got = reinterpret_cast<float *>(few_raw + Ring::kBytes + sizeof(FewShared));
     if (quad < u.rows) {
-        float *out = part + ((size_t)warp * u.rows + quad) * ds;
+        float *out = part + ((size_t)warp * u.rows + quad) * (p.d + 4) + 2 * tq;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
-            if (nt * 8 < p.d) {
-                out[nt * 8 + 2 * tq] = kSparse ? o[nt][0] + o[nt][2] : o[nt][0];
-                out[nt * 8 + 2 * tq + 1] = kSparse ? o[nt][1] + o[nt][3] : o[nt][1];
-            }
-        if (tq == 0) {
-            out[p.d] = m;
-            out[p.d + 1] = l;
-        }
+            if (nt * 8 < p.d) *reinterpret_cast<float2 *>(out + nt * 8) = kSparse ? make_float2(o[nt][0] + o[nt][2], o[nt][1] + o[nt][3]) : make_float2(o[nt][0], o[nt][1]);
+        if (tq == 0) sh.warp_stat[warp][quad] = make_float2(m, l);
     }
-    if (kSparse) few_finish<float>(part, part + (size_t)kFewWarps * kFewRows * ds, p, u);
-    else few_finish<T>(part, part + (size_t)kFewWarps * kFewRows * ds, p, u);
+    if (!kSparse) cluster_wait();   // all of the cluster has started: its shared memory may be written
+    if (kSparse) few_finish<float>(part, got, sh, p, u);
+    else few_finish<T>(part, got, sh, p, u);
 }
 
 // ------------------------------------------------------------------ f32
@@ -537,22 +599,21 @@ template <int R, int VPL, bool kSparse>
 __global__ void __launch_bounds__(kFewThreads)
 few_fma_kernel(const __grid_constant__ FewParams p, int lpk)
 {
+    cluster_arrive();
     pdl_wait();
     pdl_release();
     constexpr int VE = 4, KT = 4;
-    extern __shared__ __align__(16) uint8_t few_raw[];   // the selection, then [warps][R][d + 2] and [R][d + 2]
+    extern __shared__ __align__(16) uint8_t few_raw[];   // FewShared, the blocks' shares of the result, the warps' results (and before them the scores)
     const FewUnit u(p);
-    BlockSelection *sel = reinterpret_cast<BlockSelection *>(few_raw);
-    float *part = reinterpret_cast<float *>(few_raw + (kSparse ? sizeof(BlockSelection) : 0));
-    int selected = 0;
-    if (kSparse) {
-        cluster_sync();
-        selected = select_blocks<float>(*sel, reinterpret_cast<double *>(part), p, u);
-        if (p.list && u.rank == 0 && u.row0 == 0)
-            for (int i = threadIdx.x; i < p.blocks; i += kFewThreads) p.list[(size_t)blockIdx.y * p.blocks + i] = i < selected ? sel->list[i] : -1;
-    } else if (u.rows <= 0) {
+    FewShared &sh = *reinterpret_cast<FewShared *>(few_raw);
+    float *got = reinterpret_cast<float *>(few_raw + sizeof(FewShared)), *part = got + R * p.d + 4 * kFewMaxRanks;
+    if (!kSparse && u.rows <= 0) {   // (the whole cluster)
+        cluster_wait();
         return;
     }
+    const int selected = kSparse ? select_blocks<float>(sh, reinterpret_cast<double *>(part), p, u) : 0;
+    if (kSparse && p.list && u.rank == 0 && u.row0 == 0)
+        for (int i = threadIdx.x; i < p.blocks; i += kFewThreads) p.list[(size_t)blockIdx.y * p.blocks + i] = i < selected ? sh.list[i] : -1;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, vecs = p.d / VE;
     const int gpw = 32 / lpk, gq = lane / lpk, gl = lane - gq * lpk, ng = kFewWarps * gpw, grp = warp * gpw + gq;
     const float4 *K = reinterpret_cast<const float4 *>((const float *)p.K + (size_t)u.unit * p.unit_rows * p.d);
@@ -594,7 +655,7 @@ few_fma_kernel(const __grid_constant__ FewParams p, int lpk)
             const float4 *ka = K, *va = V;
             if (i < last) {
                 if (kSparse) {
-                    const int row = sel->list[i / p.block_rows] * p.block_rows + i % p.block_rows;
+                    const int row = sh.list[i / p.block_rows] * p.block_rows + i % p.block_rows;
                     if (row < p.len) {
                         seen_by[j] = 0;
                         ka = K + (size_t)row * vecs;
@@ -677,29 +738,20 @@ few_fma_kernel(const __grid_constant__ FewParams p, int lpk)
             }
         }
     }
-    const int ds = p.d + 2;
+    __syncthreads();   // (the scores' place)
     if (gq == 0) {
 #pragma unroll
         for (int h = 0; h < R; ++h) {
             if (h >= u.rows) break;
-            float *row = part + ((size_t)warp * u.rows + h) * ds;
+            float4 *row = reinterpret_cast<float4 *>(part + ((size_t)warp * u.rows + h) * (p.d + 4));
 #pragma unroll
-            for (int x = 0; x < VPL; ++x) {
-                const int v = gl + x * lpk;
-                if (v < vecs) {
-                    row[v * VE] = acc[h][x].x;
-                    row[v * VE + 1] = acc[h][x].y;
-                    row[v * VE + 2] = acc[h][x].z;
-                    row[v * VE + 3] = acc[h][x].w;
-                }
-            }
-            if (gl == 0) {
-                row[p.d] = m[h];
-                row[p.d + 1] = l[h];
-            }
+            for (int x = 0; x < VPL; ++x)
+                if (gl + x * lpk < vecs) row[gl + x * lpk] = acc[h][x];
+            if (gl == 0) sh.warp_stat[warp][h] = make_float2(m[h], l[h]);
         }
     }
-    few_finish<float>(part, part + (size_t)kFewWarps * R * ds, p, u);
+    if (!kSparse) cluster_wait();   // all of the cluster has started: its shared memory may be written
+    few_finish<float>(part, got, sh, p, u);
 }
 
 // ------------------------------------------------------------------ host side
@@ -714,35 +766,41 @@ inline cudaError_t launch_few_t(void (*kern)(FewParams, A...), const FewParams &
 template <int R, int VPL, bool kSparse>
 inline cudaError_t launch_few_fma(const FewParams &p, int lpk, int cluster, cudaStream_t stream)
 {
-    size_t smem = (size_t)(kFewWarps + 1) * R * (p.d + 2) * sizeof(float);
-    if (kSparse) smem = sizeof(BlockSelection) + (smem > kFewBlocks * sizeof(double) ? smem : kFewBlocks * sizeof(double));
-    return launch_few_t<int>(few_fma_kernel<R, VPL, kSparse>, p, smem, cluster, stream, lpk);
+    size_t part = (size_t)kFewWarps * R * (p.d + 4) * sizeof(float);
+    if (kSparse && part < kFewBlocks * sizeof(double)) part = kFewBlocks * sizeof(double);
+    return launch_few_t<int>(few_fma_kernel<R, VPL, kSparse>, p, sizeof(FewShared) + (R * p.d + 4 * kFewMaxRanks) * sizeof(float) + part, cluster, stream, lpk);
 }
 
 template <int D, bool kSparse>
 inline cudaError_t launch_few_mma(const FewParams &p, int cluster, cudaStream_t stream)
 {
-    return launch_few_t<>(few_mma_kernel<D, kSparse>, p, FewRing<D>::kBytes + (kSparse ? sizeof(BlockSelection) : 0), cluster, stream);
+    using Ring = FewRing<D>;
+    return launch_few_t<>(few_mma_kernel<D, kSparse>, p, Ring::kBytes + sizeof(FewShared) + Ring::kGot, cluster, stream);
 }
 
 template <bool kSparse>
 inline cudaError_t launch_few(const FewParams &p, bool f32, int sm_count, cudaStream_t stream)
 {
-    // blocks of a cluster: as many as find a place at once (two on an SM), and at least one tile of 16 keys for every warp
+    // blocks of a cluster: as many as find a place at once (two on an SM), and at least one tile of 16 keys for every warp.  (8 warps a block, one on an
+    // SM: a cluster of 16 then needs 16 SMs of one GPC to itself, and 8 of them do not run side by side: one token over 4095 rows, 8 units 13.8 us against 8.9.)
     const long long units = (long long)p.layers * p.streams * p.Hkv * ((p.n * p.G + kFewRows - 1) / kFewRows);
     const int keys = kSparse ? (p.len < p.blocks * p.block_rows ? p.len : p.blocks * p.block_rows) : p.len + p.n;
     int cluster = 1;
-    while (cluster < 16 && units * cluster * 2 <= 2LL * sm_count && keys > cluster * 16 * kFewWarps) cluster *= 2;
-    if (!f32) return p.d <= 64 ? launch_few_mma<64, kSparse>(p, cluster, stream) : p.d <= 128 ? launch_few_mma<128, kSparse>(p, cluster, stream) : launch_few_mma<256, kSparse>(p, cluster, stream);
+    while (cluster < kFewMaxRanks && units * cluster * 2 <= 2LL * sm_count && keys > cluster * 16 * kFewWarps) cluster *= 2;
+    if (!f32) {
+        if (p.d <= 64) return launch_few_mma<64, kSparse>(p, cluster, stream);
+        return p.d <= 128 ? launch_few_mma<128, kSparse>(p, cluster, stream) : launch_few_mma<256, kSparse>(p, cluster, stream);
+    }
     const int vecs = p.d / 4, rows = p.n * p.G;
     int lpk = 1;
     while (lpk < vecs && lpk < 32) lpk *= 2;
-    if (vecs > 32)
-        return rows == 1 ? launch_few_fma<1, 2, kSparse>(p, lpk, cluster, stream) : rows <= 4 ? launch_few_fma<4, 2, kSparse>(p, lpk, cluster, stream)
-                                                                                             : launch_few_fma<8, 2, kSparse>(p, lpk, cluster, stream);
-    return rows == 1 ? launch_few_fma<1, 1, kSparse>(p, lpk, cluster, stream) : rows == 2 ? launch_few_fma<2, 1, kSparse>(p, lpk, cluster, stream)
-         : rows <= 4 ? launch_few_fma<4, 1, kSparse>(p, lpk, cluster, stream)
-                                                                                         : launch_few_fma<8, 1, kSparse>(p, lpk, cluster, stream);
+    if (vecs > 32) {
+        if (rows == 1) return launch_few_fma<1, 2, kSparse>(p, lpk, cluster, stream);
+        return rows <= 4 ? launch_few_fma<4, 2, kSparse>(p, lpk, cluster, stream) : launch_few_fma<8, 2, kSparse>(p, lpk, cluster, stream);
+    }
+    if (rows == 1) return launch_few_fma<1, 1, kSparse>(p, lpk, cluster, stream);
+    if (rows == 2) return launch_few_fma<2, 1, kSparse>(p, lpk, cluster, stream);
+    return rows <= 4 ? launch_few_fma<4, 1, kSparse>(p, lpk, cluster, stream) : launch_few_fma<8, 1, kSparse>(p, lpk, cluster, stream);
 }
 
 }  // namespace ipotk
