@@ -421,7 +421,8 @@ int ipot_view_blocks(ipot_t *pot, void **lo, void **hi, int *n_blocks);
  * row, and of the others the n_blocks - 1 with the largest
  *   s_b = sum over the unit's query heads of sum_c max(q_c lo_bc, q_c hi_bc),
  * which no head's logit sum over a row of the block exceeds (ties: the lower block; evaluated in 64 bits).  The heads of a unit share the selection.
- *   q, out, lse : as for ipot_decode_attention, with n_layers in place of layers; the softmax is taken over the selected rows
+ *   q, out, lse : as for ipot_decode_attention, with n_layers in place of layers (out 16-byte aligned); the softmax is taken over the
+ *                 selected rows
  *   blocks      : device int32 [n_layers][batch][Hkv][n_blocks], or NULL: the chosen blocks in ascending order, -1 behind the last
  *                 where the pot has fewer than n_blocks blocks (all are then chosen)
  * Everything is fp32 where not said otherwise.  All inputs must be finite.  Asynchronous on the pot's stream; the pot is not changed.

@@ -1224,7 +1224,7 @@ int ipot_view_blocks(ipot_t *p, void **lo, void **hi, int *n_blocks)
 
 int ipot_decode_attention_blocks(ipot_t *p, int layer, int n_layers, const void *q, int n_blocks, float *out, float *lse, int32_t *blocks)
 {
-    if (!p || !q || !out || !aligned16(q) || ((reinterpret_cast<uintptr_t>(out) | reinterpret_cast<uintptr_t>(lse) | reinterpret_cast<uintptr_t>(blocks)) & 3u))
+    if (!p || !q || !out || !aligned16(q) || !aligned16(out) || ((reinterpret_cast<uintptr_t>(lse) | reinterpret_cast<uintptr_t>(blocks)) & 3u))
         return IPOT_E_INVALID;
     if (layer < 0 || n_layers < 1 || layer > p->cfg.layers - n_layers || n_blocks < 1) return IPOT_E_INVALID;
     if (!p->blk_rows) return IPOT_E_STATE;

@@ -36,6 +36,13 @@ __device__ __forceinline__ float few_scale(float m, float ref) { return m == -IN
 constexpr int kFewThreads = 128, kFewWarps = kFewThreads / 32, kFewMaxRanks = 16;
 constexpr int kFewRows = 8;       // query rows of a block
 constexpr int kFewBlocks = 2048;  // blocks of a unit: 32768 slots, 16 rows
+constexpr int kScoreBytes = kFewBlocks * (int)sizeof(double);
+constexpr int kFewFmaRoom = 64 * 1024;   // for bounds (few_fma_kernel; the others have their ring)
+
+__device__ __forceinline__ void few_cp_async16(void *dst, const void *src, bool there)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
 
 // What a block works on, and what its threads know of it.
 struct FewUnit {
@@ -187,12 +194,14 @@ __device__ __forceinline__ void select_in_block(FewShared &sh, const double *sco
     }
 }
 
-// All blocks of the cluster: sh.list becomes the ascending list of the chosen blocks, its length is returned.  score: kFewBlocks numbers of
-// shared memory that is free meanwhile, at the same place in every block.  The cluster has arrived at its first barrier.
+// All blocks of the cluster: sh.list becomes the ascending list of the chosen blocks, its length is returned.  free_bytes: shared memory that is free
+// meanwhile, room_bytes behind kFewBlocks scores, at the same place in every block.  The cluster has arrived at its first barrier.
 template <typename T>
-__device__ __forceinline__ int select_blocks(FewShared &sh, double *score, const FewParams &p, const FewUnit &u)
+__device__ __forceinline__ int select_blocks(FewShared &sh, uint8_t *free_bytes, int room_bytes, const FewParams &p, const FewUnit &u)
 {
-    constexpr int VE = RowVec<T>::kElems, NV = sizeof(T) == 2 ? 2 : 4;   // 256 channels: 64 vectors of bf16 bounds, 128 of f32
+    double *score = reinterpret_cast<double *>(free_bytes);
+    RowVec<T> *bounds = reinterpret_cast<RowVec<T> *>(score + kFewBlocks);
+    constexpr int VE = RowVec<T>::kElems, NV = sizeof(T) == 2 ? 2 : 4, BF = 4;   // 256 channels: 64 vectors of bf16 bounds, 128 of f32
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, vecs = p.d / VE, pieces = 2 * vecs;
     const int total = (p.len + p.block_rows - 1) / p.block_rows, want = min(p.blocks, total), others = total - 1, need = want - 1;
     if (want == total || need == 0) {
@@ -201,23 +210,20 @@ __device__ __forceinline__ int select_blocks(FewShared &sh, double *score, const
         cluster_wait();
         return want;
     }
-    // this lane's channels: vector lane + 32 i of a block's lower, then upper bounds
+    // this block's share of the others: their bounds come into shared memory, as many at once as find room.  (Straight into registers, four blocks a warp and four more on their
+    // way, the loads were a chain of latencies: 256 units x 127 blocks x 128 channels 41 us for the call, 33 so.)
     const T *lo = (const T *)p.lo + (size_t)u.unit * p.unit_blocks * p.d, *hi = (const T *)p.hi + (size_t)u.unit * p.unit_blocks * p.d;
-    constexpr int BF = 4;   // blocks whose bounds are on their way at once
-    const int stride = u.ranks * kFewWarps;
-    RowVec<T> x[BF][NV], x_next[BF][NV];
-    auto fetch = [&](RowVec<T> (&x)[BF][NV], int b0) {
-#pragma unroll
-        for (int f = 0; f < BF; ++f)
-#pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int piece = lane + 32 * i, b = min(b0 + f * stride, others - 1);
-                const bool upper = piece >= vecs;
-                if (piece < pieces) x[f][i] = *reinterpret_cast<const RowVec<T> *>((upper ? hi : lo) + (size_t)b * p.d + (piece - (upper ? vecs : 0)) * VE);
-            }
+    const int mine0 = (int)((long long)others * u.rank / u.ranks), mine = (int)((long long)others * (u.rank + 1) / u.ranks) - mine0, room = room_bytes / (2 * p.d * (int)sizeof(T));
+    auto fetch = [&](int from) {
+        const int n = min(room, mine - from) * vecs;
+        const RowVec<T> *l = reinterpret_cast<const RowVec<T> *>(lo + (size_t)(mine0 + from) * p.d), *h = reinterpret_cast<const RowVec<T> *>(hi + (size_t)(mine0 + from) * p.d);
+        for (int e = threadIdx.x; e < n; e += kFewThreads) {
+            few_cp_async16(bounds + e, l + e, true);
+            few_cp_async16(bounds + room * vecs + e, h + e, true);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    int b0 = u.rank * kFewWarps + warp;
-    fetch(x, b0);
+    fetch(0);
     // what the heads' queries sum up to in those channels, above and below zero
     double w[NV * VE];
     const T *q = (const T *)p.q + u.l * p.qs.layer + u.b * p.qs.stream + (long long)u.hkv * p.G * p.qs.head;
@@ -244,44 +250,50 @@ __device__ __forceinline__ int select_blocks(FewShared &sh, double *score, const
         }
     }
     cluster_wait();   // all of the cluster has started: its shared memory may be written
-    for (;;) {
-        const bool more = b0 + BF * stride < others;
-        if (more) fetch(x_next, b0 + BF * stride);
-        double sum[BF];   // of four blocks side by side: the chains of 64-bit sums are long
+    for (int from = 0; from < mine; from += room) {
+        if (from) {
+            __syncthreads();
+            fetch(from);
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncthreads();
+        const int n = min(room, mine - from);
+        for (int i0 = warp; i0 < n; i0 += BF * kFewWarps) {
+            double sum[BF];   // of four blocks side by side: the chains of 64-bit sums are long
 #pragma unroll
-        for (int f = 0; f < BF; ++f) sum[f] = 0.0;
+            for (int f = 0; f < BF; ++f) sum[f] = 0.0;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-            if (lane + 32 * i < pieces) {
+            for (int i = 0; i < NV; ++i)
+                if (lane + 32 * i < pieces) {
+                    const int piece = lane + 32 * i;
+                    const RowVec<T> *at = bounds + (piece >= vecs ? room * vecs + piece - vecs : piece);
+                    RowVec<T> x[BF];
 #pragma unroll
-                for (int e = 0; e < VE; ++e)
+                    for (int f = 0; f < BF; ++f) x[f] = at[min(i0 + f * kFewWarps, n - 1) * vecs];
 #pragma unroll
-                    for (int f = 0; f < BF; ++f) sum[f] = fma(w[i * VE + e], (double)to_float(x[f][i].e[e]), sum[f]);
+                    for (int e = 0; e < VE; ++e)
+#pragma unroll
+                        for (int f = 0; f < BF; ++f) sum[f] = fma(w[i * VE + e], (double)to_float(x[f].e[e]), sum[f]);
+                }
+            // sums over the lanes: a lane keeps half of what it has and sends the other half, so that lanes 8 f .. 8 f + 7 end with block f's
+            static_assert(BF == 4, "two halvings");
+            {
+                const bool up = lane & 16;
+                const double s0 = __shfl_xor_sync(0xffffffffu, up ? sum[0] : sum[2], 16), s1 = __shfl_xor_sync(0xffffffffu, up ? sum[1] : sum[3], 16);
+                sum[0] = (up ? sum[2] : sum[0]) + s0;
+                sum[1] = (up ? sum[3] : sum[1]) + s1;
             }
-        // sums over the lanes: a lane keeps half of what it has and sends the other half, so that lanes 8 f .. 8 f + 7 end with block f's
-        static_assert(BF == 4, "two halvings");
-        {
-            const bool up = lane & 16;
-            const double s0 = __shfl_xor_sync(0xffffffffu, up ? sum[0] : sum[2], 16), s1 = __shfl_xor_sync(0xffffffffu, up ? sum[1] : sum[3], 16);
-            sum[0] = (up ? sum[2] : sum[0]) + s0;
-            sum[1] = (up ? sum[3] : sum[1]) + s1;
+            {
+                const bool up = lane & 8;
+                const double s0 = __shfl_xor_sync(0xffffffffu, up ? sum[0] : sum[1], 8);
+                sum[0] = (up ? sum[1] : sum[0]) + s0;
+            }
+#pragma unroll
+            for (int off = 4; off >= 1; off >>= 1) sum[0] += __shfl_xor_sync(0xffffffffu, sum[0], off);
+            const int i = i0 + (lane >> 3) * kFewWarps;
+            if (i < n)
+                for (uint32_t r = lane & 7; r < u.ranks; r += 8) cluster_st(cluster_addr(score + mine0 + from + i, r), sum[0]);
         }
-        {
-            const bool up = lane & 8;
-            const double s0 = __shfl_xor_sync(0xffffffffu, up ? sum[0] : sum[1], 8);
-            sum[0] = (up ? sum[1] : sum[0]) + s0;
-        }
-#pragma unroll
-        for (int off = 4; off >= 1; off >>= 1) sum[0] += __shfl_xor_sync(0xffffffffu, sum[0], off);
-        const int b = b0 + (lane >> 3) * stride;
-        if (b < others)
-            for (uint32_t r = lane & 7; r < u.ranks; r += 8) cluster_st(cluster_addr(score + b, r), sum[0]);
-        if (!more) break;
-        b0 += BF * stride;
-#pragma unroll
-        for (int f = 0; f < BF; ++f)
-#pragma unroll
-            for (int i = 0; i < NV; ++i) x[f][i] = x_next[f][i];
     }
     cluster_sync();
     if (others <= 2 * kFewThreads) select_in_block<2>(sh, score, others, need);
@@ -293,7 +305,9 @@ __device__ __forceinline__ int select_blocks(FewShared &sh, double *score, const
 
 // ------------------------------------------------------------------ the end of a block's work
 // part: [warps][rows][d + 4] outputs against the references in sh.warp_stat; got: room for the blocks' shares of the result.
-template <typename O>
+// kAlone: with a way of its own for a block that is its own cluster, which has much for few threads (selected blocks of 256 units 38.4 -> 36.6 us).  Its code costs launches of few
+// units, which never come there, 0.6 of 7.3 us: a single token's few microseconds are worth more than 2 of the 80 that many units take.
+template <typename O, bool kAlone>
 __device__ __forceinline__ void few_finish(float *part, float *got, FewShared &sh, const FewParams &p, const FewUnit &u)
 {
     const int ds = p.d + 4, all = u.rows * p.d, share = ((all + (int)u.ranks - 1) / (int)u.ranks + 3) & ~3;
@@ -324,6 +338,23 @@ __device__ __forceinline__ void few_finish(float *part, float *got, FewShared &s
         cluster_st(cluster_addr(got + u.rank * share + e - owner * share, owner), v);
     }
     cluster_sync();   // from here on a block touches its own memory alone
+    if (kAlone && u.ranks == 1) {
+        for (int e = threadIdx.x * 4; e < all; e += kFewThreads * 4) {
+            const int h = e / p.d, c = e - h * p.d, t = (u.row0 + h) / p.G, g = u.hkv * p.G + u.row0 + h - t * p.G;
+            const float2 st = sh.stat[0][h];
+            const float4 x = *reinterpret_cast<const float4 *>(got + e);
+            struct alignas(4 * sizeof(O)) Four {
+                O e[4];
+            } out;
+            out.e[0] = from_float<O>(x.x / st.y);
+            out.e[1] = from_float<O>(x.y / st.y);
+            out.e[2] = from_float<O>(x.z / st.y);
+            out.e[3] = from_float<O>(x.w / st.y);
+            *reinterpret_cast<Four *>((O *)p.out + u.l * p.os.layer + u.b * p.os.stream + g * p.os.head + (long long)t * p.os.token + c) = out;
+            if (c == 0 && p.lse) p.lse[(((size_t)u.l * p.streams + u.b) * p.Hkv * p.G + g) * p.n + t] = 0.6931471805599453f * (st.x + log2f(st.y));
+        }
+        return;
+    }
     for (int i = threadIdx.x; i < share; i += kFewThreads) {
         const int e = u.rank * share + i;
         if (e >= all) break;
@@ -332,7 +363,7 @@ __device__ __forceinline__ void few_finish(float *part, float *got, FewShared &s
         float2 st[kFewMaxRanks];
         float x[kFewMaxRanks];
 #pragma unroll
-        for (uint32_t r = 0; r < kFewMaxRanks; ++r) {
+        for (uint32_t r = 0; r < kFewMaxRanks; ++r) {   // all reads at once
             st[r] = make_float2(-INFINITY, 0.f);
             x[r] = 0.f;
             if (r < u.ranks) {
@@ -385,13 +416,9 @@ constexpr int kFewStages = 3;
 template <int D> struct FewRing {
     static constexpr size_t kBytes = (size_t)kFewWarps * kFewStages * 2 * 16 * D * 2;
     static constexpr size_t kGot = (kFewRows * D + 4 * kFewMaxRanks) * sizeof(float);
-    static_assert(kBytes >= kFewBlocks * sizeof(double) && kBytes >= kFewWarps * kFewRows * (D + 4) * sizeof(float), "scores and the merge take its place");
+    static_assert(kBytes >= kScoreBytes + 8 * 1024 && kBytes >= kFewWarps * kFewRows * (D + 4) * sizeof(float), "scores and the merge take its place");
 };
 
-__device__ __forceinline__ void few_cp_async16(void *dst, const void *src, bool there)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
 __device__ __forceinline__ void few_ldmatrix(uint32_t (&r)[4], uint32_t addr)
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr));
@@ -444,7 +471,7 @@ few_mma_kernel(const __grid_constant__ FewParams p)
                 qa[ks][x] = quad < u.rows && c < p.d ? __ldg(reinterpret_cast<const uint32_t *>(qr + c)) : 0u;
             }
     }
-    const int selected = kSparse ? select_blocks<T>(sh, reinterpret_cast<double *>(few_raw), p, u) : 0;
+    const int selected = kSparse ? select_blocks<T>(sh, few_raw, (int)Ring::kBytes - kScoreBytes, p, u) : 0;
     const FewTiles<kSparse> tiles(p, u, selected);
     const uint4 *K = reinterpret_cast<const uint4 *>((const T *)p.K + (size_t)u.unit * p.unit_rows * p.d);
     const uint4 *V = reinterpret_cast<const uint4 *>((const T *)p.V + (size_t)u.unit * p.unit_rows * p.d);
@@ -589,8 +616,8 @@ few_mma_kernel(const __grid_constant__ FewParams p)
         if (tq == 0) sh.warp_stat[warp][quad] = make_float2(m, l);
     }
     if (!kSparse) cluster_wait();   // all of the cluster has started: its shared memory may be written
-    if (kSparse) few_finish<float>(part, got, sh, p, u);
-    else few_finish<T>(part, got, sh, p, u);
+    if (kSparse) few_finish<float, true>(part, got, sh, p, u);
+    else few_finish<T, false>(part, got, sh, p, u);
 }
 
 // ------------------------------------------------------------------ f32
@@ -611,7 +638,7 @@ few_fma_kernel(const __grid_constant__ FewParams p, int lpk)
         cluster_wait();
         return;
     }
-    const int selected = kSparse ? select_blocks<float>(sh, reinterpret_cast<double *>(part), p, u) : 0;
+    const int selected = kSparse ? select_blocks<float>(sh, reinterpret_cast<uint8_t *>(part), kFewFmaRoom, p, u) : 0;
     if (kSparse && p.list && u.rank == 0 && u.row0 == 0)
         for (int i = threadIdx.x; i < p.blocks; i += kFewThreads) p.list[(size_t)blockIdx.y * p.blocks + i] = i < selected ? sh.list[i] : -1;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, vecs = p.d / VE;
@@ -751,7 +778,7 @@ few_fma_kernel(const __grid_constant__ FewParams p, int lpk)
         }
     }
     if (!kSparse) cluster_wait();   // all of the cluster has started: its shared memory may be written
-    few_finish<float>(part, got, sh, p, u);
+    few_finish<float, kSparse>(part, got, sh, p, u);
 }
 
 // ------------------------------------------------------------------ host side
@@ -767,7 +794,7 @@ template <int R, int VPL, bool kSparse>
 inline cudaError_t launch_few_fma(const FewParams &p, int lpk, int cluster, cudaStream_t stream)
 {
     size_t part = (size_t)kFewWarps * R * (p.d + 4) * sizeof(float);
-    if (kSparse && part < kFewBlocks * sizeof(double)) part = kFewBlocks * sizeof(double);
+    if (kSparse && part < kScoreBytes + kFewFmaRoom) part = kScoreBytes + kFewFmaRoom;
     return launch_few_t<int>(few_fma_kernel<R, VPL, kSparse>, p, sizeof(FewShared) + (R * p.d + 4 * kFewMaxRanks) * sizeof(float) + part, cluster, stream, lpk);
 }
 

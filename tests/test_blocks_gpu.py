@@ -266,7 +266,7 @@ def test_refusals():
         cos = torch.ones((100, 32), device="cuda").bfloat16()
         assert L.ipot_enable_rope(h, cos.data_ptr(), cos.data_ptr(), 1) == ipot.IPOT_E_STATE   # the bounds would be those of other keys
         ipot.ipot_append_chunk(h, K, K, 20)
-        for kw in (dict(h=None), dict(q=None), dict(out=None), dict(q=q.data_ptr() + 8), dict(out=out.data_ptr() + 2), dict(lse=out.data_ptr() + 1), dict(blocks=out.data_ptr() + 2),
+        for kw in (dict(h=None), dict(q=None), dict(out=None), dict(q=q.data_ptr() + 8), dict(out=out.data_ptr() + 2), dict(out=out.data_ptr() + 4), dict(lse=out.data_ptr() + 1), dict(blocks=out.data_ptr() + 2),
                    dict(layer=-1), dict(layers=0), dict(layer=1), dict(n=0), dict(n=8), dict(n=-1)):
             assert rc(**kw) == ipot.IPOT_E_INVALID, kw
         assert ipot.ipot_sync_status(h) == 0 and bool((out == 0).all())
