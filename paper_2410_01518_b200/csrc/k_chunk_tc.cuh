@@ -4,8 +4,12 @@
 // rows of floor(128 / G) tokens (TMA fetches it as a box of G heads x tokens, whatever the strides).  Keys come in tiles of KT,
 // first the pot's, then the chunk's.  Per tile and stream
 //   S = Q K^T   128 x KT fp32 in tensor memory (both operands in shared memory, K-major, 128-byte swizzle)
-//   softmax     a thread owns a row: p = 2^(s c - m) against a reference m that is only moved when the row's maximum passes it by
-//               2^8 (then the row's sums and output are scaled down: rare), l += p in fp32, and p as bf16 over S in tensor memory
+//   softmax     a thread owns half of a row (one warp per scheduler and stream would be a chain of latencies: 1900 cycles a tile, two 1000): p = 2^(s c - m),
+//               l += p in fp32, and p as bf16 over S in tensor memory.  The reference m is the maximum of the
+//               row's first tile; after that no maximum is taken.  fp32 and bf16 have the same exponents, so p is as exact far above 1 as below,
+//               and only a tile whose sum passes 2^60 moves the reference (the row's sums and output are then scaled down: rare).  All exponentials are the
+//               special-function unit's: a quarter of them as a polynomial on the FMA pipe took 1016 us for 4 streams x 2048 tokens over 6144 rows instead of 950
+//               (in long runs the power limit holds the clock at 1.6 GHz, and what is issued costs power).
 //   O += P V    P from tensor memory, V as it lies (channels contiguous: the N-major operand layout), 128 x D fp32 in tensor memory
 // A block runs two streams so that the tensor core works on one while the other's softmax runs: two query tiles that share the
 // key tiles (kSplit = false), or one query tile whose key tiles take turns (kSplit, for calls of few rows; merged at the
@@ -13,7 +17,10 @@
 // SMs spread a tile's keys over a cluster whose blocks merge their results through distributed shared memory: nothing is
 // exchanged through global memory, and the result does not depend on timing.
 //
-// Warps: 0 loads (TMA), 1 issues the products, 2-5 / 6-9 softmax of the two streams.  All waits are bounded (wait_ns): one that runs out
+// Warps: 0 loads (TMA), 1 issues the products, 2-9 / 10-17 softmax of the two streams (2-5, 10-13 the left half of the columns).  Between two streams' products the issuing warp waits for nothing but
+// the next P: every look at a barrier costs about 90 cycles even if it has long been passed, and the tensor core's queue is shorter than that.
+// (A warp for each stream's products: 1140 us against 1020 for 4 streams x 2048 tokens over 6144 rows, their products then alternate one by one and both are late.)
+// All waits are bounded (wait_ns): one that runs out
 // raises the block's give-up flag and IPOT_E_TIMEOUT; from then on nothing more is put in flight, and what is in flight is
 // waited for before tensor memory is released.
 #pragma once
@@ -25,7 +32,7 @@
 namespace ipotk {
 
 constexpr int kCtRows = 128;
-constexpr float kChunkSlack = 8.f;   // binary orders by which a row's maximum may pass its reference
+constexpr float kChunkMost = 1.1529215e18f;   // 2^60: a tile's sum of a row up to here leaves the reference where it is
 
 template <int D, bool kSplit> struct ChunkTc {
     static constexpr int kStreams = D > 128 ? 1 : 2;
@@ -39,11 +46,12 @@ template <int D, bool kSplit> struct ChunkTc {
     static constexpr uint32_t kOffStage = 0, kOffQ = kStages * kStageBytes, kOffStat = kOffQ + kQTiles * kQBytes;   // [2][128] float2
     static constexpr uint32_t kOffBar = kOffStat + kStreams * kCtRows * 8, kOffFlag = kOffBar + 8 * 32, kSmemBytes = kOffFlag + 16;
     static constexpr uint32_t kOutCol = 256;                                 // tensor memory: S of stream i at 128 i, O at 256 + D i
-    static constexpr int kThreads = 64 + 128 * kStreams;
+    static constexpr int kThreads = 64 + 256 * kStreams;
+    static constexpr int kCols = kKeys / 2;                                  // of a softmax thread
     static_assert(kStreams * kCtRows * kPitch * 4 <= kStages * kStageBytes, "partial results take the stages' place");
     static_assert(kSmemBytes <= 232448, "shared memory of a block");
 };
-enum { kCbQ = 0, kCbFull = 1, kCbEmpty = 9, kCbS = 17, kCbP = 19, kCbO = 21, kCbDrain = 23 };
+enum { kCbQ = 0, kCbFull = 1, kCbEmpty = 9, kCbS = 17, kCbP = 19, kCbO = 21, kCbDrain = 23, kCbCount = 24 };
 
 // D[M x N] += A B with A in tensor memory (a row per lane, two bf16 per column).
 __device__ __forceinline__ void tc_mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
@@ -97,6 +105,98 @@ __device__ __forceinline__ bool chunk_wait(uint32_t bar, uint32_t parity, volati
     }
 }
 
+// The two warps that share 32 rows of a stream.
+__device__ __forceinline__ void chunk_pair_sync(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ bool chunk_pair_any(int id, bool x)
+{
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+        "barrier.cta.red.or.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r) : "r"((uint32_t)x), "r"(id) : "memory");
+    return r != 0;
+}
+
+// A tile of a warp's rows in general: its first (the row's maximum becomes the reference), one with columns that some row does not see, and one that left the range.
+// W columns from ts on, of which this row sees `cols`; the other warp of the pair has the other half and takes part.  seen: the row's two maxima.  scale: whether O
+// holds something already (W2 columns of it from `to` on are this warp's).  Leaves p over the first half of its columns; (reference, sum).
+template <int W, int W2>
+__device__ __noinline__ float2 chunk_tile_general(uint32_t ts, uint32_t to, int cols, float c, float m, float sum, bool valid, bool scale, float2 *seen, int half, int pair)
+{
+    float top = -INFINITY;
+#pragma unroll 1
+    for (int a = 0; a < W; a += 32) {
+        uint32_t v[32];
+        tmem_ld32(ts + a, v);
+        tmem_wait_ld(v);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) top = fmaxf(top, a + e < cols ? __uint_as_float(v[e]) : -INFINITY);
+    }
+    (half ? seen->y : seen->x) = top;
+    chunk_pair_sync(pair);
+    top = fmaxf(seen->x, seen->y) * c;
+    const bool moves = valid && top > m;
+    if (__any_sync(0xffffffffu, moves)) {   // (the same rows, the same answer in both warps)
+        const float to_m = moves ? top : m, f = moves ? chunk_ex2(m - to_m) : 1.f;   // (m = -inf: 0)
+        sum *= f;
+        m = to_m;
+        if (scale) {
+            // the product that last added to O has finished: it was issued before the one that made this tile's logits
+#pragma unroll 1
+            for (int a = 0; a < W2; a += 32) {
+                uint32_t o[32];
+                tmem_ld32(to + a, o);
+                tmem_wait_ld(o);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                tmem_st32(to + a, o);
+            }
+        }
+    }
+    const float ref = m == -INFINITY ? 0.f : m;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int a = 0; a < W; a += 32) {   // (what is stored lies in columns that have been read)
+        uint32_t v[32], h[16];
+        tmem_ld32(ts + a, v);
+        tmem_wait_ld(v);
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+            const float x = a + e < cols ? chunk_ex2(fmaf(__uint_as_float(v[e]), c, -ref)) : 0.f, y = a + e + 1 < cols ? chunk_ex2(fmaf(__uint_as_float(v[e + 1]), c, -ref)) : 0.f;
+            s[e & 2] += x;
+            s[(e & 2) + 1] += y;
+            const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
+            h[e >> 1] = *reinterpret_cast<const uint32_t *>(&b);
+        }
+        tmem_st16(ts + (a >> 1), h);
+    }
+    return make_float2(m, sum + ((s[0] + s[1]) + (s[2] + s[3])));
+}
+
+// The same for a tile that every row sees, against the reference as it is: 32 columns at a time, the next ones on their way meanwhile.  h: p, two to a register.
+template <int W>
+__device__ __forceinline__ float chunk_tile(uint32_t ts, float c, float m, uint32_t (&h)[W / 32][16])
+{
+    const float2 c2 = make_float2(c, c), r2 = make_float2(-m, -m);
+    float2 s[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+    uint32_t v[W > 32 ? 2 : 1][32];
+    tmem_ld32(ts, v[0]);
+#pragma unroll
+    for (int a = 0; a < W / 32; ++a) {
+        tmem_wait_ld(v[a & 1]);
+        if (a + 1 < W / 32) tmem_ld32(ts + 32 * (a + 1), v[(a + 1) & 1]);
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+            const float2 x = __ffma2_rn(make_float2(__uint_as_float(v[a & 1][e]), __uint_as_float(v[a & 1][e + 1])), c2, r2), w = make_float2(chunk_ex2(x.x), chunk_ex2(x.y));
+            s[(e >> 1) & 1] = __fadd2_rn(s[(e >> 1) & 1], w);
+            const __nv_bfloat162 b = __floats2bfloat162_rn(w.x, w.y);
+            h[a][e >> 1] = *reinterpret_cast<const uint32_t *>(&b);
+        }
+    }
+    const float2 t = __fadd2_rn(s[0], s[1]);
+    return t.x + t.y;
+}
+
 // grid: cluster x (row tiles or pairs of them, the longest first) x units.
 template <int D, bool kSplit>
 __global__ void __launch_bounds__(ChunkTc<D, kSplit>::kThreads, 1)
@@ -122,7 +222,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
     const int hkv = unit % p.c.Hkv, b = unit / p.c.Hkv % p.c.streams, l = unit / p.c.Hkv / p.c.streams;
     if (threadIdx.x == 0) {
         *flag = 0;
-        for (int i = 0; i < kCbDrain + 1; ++i) mbar_init(bar(i), i >= kCbP && i < kCbO ? 4 : 1);
+        for (int i = 0; i < kCbCount; ++i) mbar_init(bar(i), i >= kCbP && i < kCbO ? 8 : 1);   // (P: a stream's eight warps)
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) {
@@ -183,102 +283,73 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
         const uint32_t idesc_s = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(KT >> 3) << 17) | ((128u >> 4) << 24);
         const uint32_t idesc_o = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)((p.c.d + 15) / 16 * 2) << 17) | ((128u >> 4) << 24);
         const int ksteps = (p.c.d + 15) / 16;
-        uint32_t k = 0;   // stages used so far
         bool ok = tiles > 0, any = false;
         auto wait = [&](int which, uint32_t parity) { ok = ok && __all_sync(0xffffffffu, chunk_wait(bar(which), parity, flag, p)); };
         auto wait_stage = [&](uint32_t at) { wait(kCbFull + at % L::kStages, (at / L::kStages) & 1); };
-        auto logits = [&](int i, uint32_t at) {   // S of stream i from stage `at`
-            any = true;
-            const uint64_t a = smem_desc_sw128(base + L::kOffQ + (kSplit ? 0 : i) * L::kQBytes), bd = smem_desc_sw128(base + L::kOffStage + at % L::kStages * L::kStageBytes);
-            if (leader) {
-                for (int c = 0; c < ksteps; ++c)
-                    tc_mma_bf16(tmem + 128 * i, a + (c >> 2) * (L::kQBlk >> 4) + 2 * (c & 3), bd + (c >> 2) * (L::kKeyBlk >> 4) + 2 * (c & 3), idesc_s, c > 0);
-                tc_commit(bar(kCbS + i));
-            }
-            __syncwarp();
-        };
-        auto output = [&](int i, uint32_t at, bool more) {   // O of stream i += P V
-            any = true;
-            const uint64_t bd = smem_desc_sw128_nmajor(base + L::kOffStage + at % L::kStages * L::kStageBytes, L::kKeyBlk);
-            if (leader) {
+        const uint64_t q_desc = smem_desc_sw128(base + L::kOffQ), k_desc = smem_desc_sw128(base + L::kOffStage), v_desc = smem_desc_sw128_nmajor(base + L::kOffStage, L::kKeyBlk);
+        // (the elected lane) S of stream i from stage `at`; O of stream i += P V
+        auto logits = [&](int i, uint32_t at) {
+            const uint64_t a = q_desc + (kSplit ? 0 : i) * (L::kQBytes >> 4), b = k_desc + at % L::kStages * (L::kStageBytes >> 4);
 #pragma unroll
-                for (int c = 0; c < KT / 16; ++c)
-                    tc_mma_bf16_ts(tmem + L::kOutCol + D * i, tmem + 128 * i + 8 * c, bd + c * (16 * 128 >> 4), idesc_o, more || c > 0);
-            }
-            __syncwarp();
+            for (int c = 0; c < D / 16; ++c)
+                if (c < ksteps) tc_mma_bf16(tmem + 128 * i, a + (c >> 2) * (L::kQBlk >> 4) + 2 * (c & 3), b + (c >> 2) * (L::kKeyBlk >> 4) + 2 * (c & 3), idesc_s, c > 0);
+            tc_commit(bar(kCbS + i));
         };
-        auto release = [&](uint32_t at) {
-            if (leader) tc_commit(bar(kCbEmpty + at % L::kStages));
-            __syncwarp();
+        auto output = [&](int i, uint32_t at, bool more) {
+            const uint64_t b = v_desc + at % L::kStages * (L::kStageBytes >> 4);
+#pragma unroll
+            for (int c = 0; c < KT / 16; ++c)
+                tc_mma_bf16_ts(tmem + L::kOutCol + D * i, tmem + 128 * i + (c >= KT / 32 ? L::kCols - 8 * (KT / 32) : 0) + 8 * c, b + c * (16 * 128 >> 4), idesc_o, more || c > 0);
         };
+        auto release = [&](uint32_t at) { tc_commit(bar(kCbEmpty + at % L::kStages)); };
         // Values behind a stream's last token count for nothing but must be finite: 0 times what lies there is not 0 otherwise.
-        auto clear_padding = [&](int t, uint32_t at) {
-            const int tile = first + t, from = n - (tile - pot_tiles) * KT;
-            if (tile < pot_tiles || from >= KT || n == p.c.n) return;
+        const int ragged = n < p.c.n && n % KT ? pot_tiles + n / KT - first : -1;   // the tile that has some
+        auto clear_padding = [&](uint32_t at) {
             uint8_t *v = ct_raw + L::kOffStage + at % L::kStages * L::kStageBytes;
             for (int h = 0; h < L::kHalves; ++h)
-                for (int e = from * 8 + lane; e < KT * 8; e += 32) *reinterpret_cast<uint4 *>(v + h * L::kKeyBlk + e * 16) = make_uint4(0, 0, 0, 0);
+                for (int e = n % KT * 8 + lane; e < KT * 8; e += 32) *reinterpret_cast<uint4 *>(v + h * L::kKeyBlk + e * 16) = make_uint4(0, 0, 0, 0);
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
         };
+        // keys and values of tile t were the how-manyth load (see there)
+        constexpr int ahead = kSplit ? S : 1;
+        auto keys_at = [&](int t) { return (uint32_t)(t < ahead ? t : 2 * t - ahead + 1); };
+        auto values_at = [&](int t) { return (uint32_t)(min(ahead, tiles) + t + min(t, max(0, tiles - ahead))); };
+        const int live = kSplit ? S : tokens[1] > 0 ? 2 : 1;   // streams
         wait(kCbQ, 0);
-        if (kSplit) {
-            for (int t = 0; t < min(S, tiles) && ok; ++t, ++k) {
-                wait_stage(k);
-                if (!ok) break;
-                tc_fence_after();
-                logits(t, k);
-                release(k);
+        for (int t = 0; t < min(ahead, tiles); ++t) {
+            wait_stage(keys_at(t));
+            if (!ok) break;
+            any = true;
+            tc_fence_after();
+            if (leader) {
+                for (int i = kSplit ? t : 0; i < (kSplit ? t + 1 : live); ++i) logits(i, keys_at(t));
+                release(keys_at(t));
             }
-            for (int t = 0; t < tiles && ok; ++t) {
-                const int i = t % S;
-                wait_stage(k);
-                wait(kCbP + i, (t / S) & 1);
+            __syncwarp();
+        }
+        for (int t = 0; t < tiles && ok; ++t) {
+            const uint32_t at = values_at(t);
+            const bool more = t + ahead < tiles;
+            wait_stage(at);
+            if (more) wait_stage(at + 1);   // the keys loaded next
+            if (ok && t == ragged) clear_padding(at);
+            for (int i = kSplit ? t % S : 0; i < (kSplit ? t % S + 1 : live); ++i) {
+                wait(kCbP + i, (kSplit ? t / S : t) & 1);
                 if (!ok) break;
                 tc_fence_after();
-                clear_padding(t, k);
-                output(i, k, t >= S);
-                release(k++);
-                if (t + S < tiles) {
-                    wait_stage(k);
-                    if (!ok) break;
-                    logits(i, k);
-                    release(k++);
-                } else if (leader) {
-                    tc_commit(bar(kCbO + i));
+                if (leader) {
+                    output(i, at, t >= ahead);
+                    if (more) logits(i, at + 1);
+                    else tc_commit(bar(kCbO + i));
                 }
                 __syncwarp();
             }
-        } else {
-            const int live = tokens[1] > 0 ? 2 : 1;
-            wait_stage(0);
-            tc_fence_after();
-            for (int i = 0; i < live && ok; ++i) logits(i, 0);
-            if (ok) release(0);
-            k = 1;
-            for (int t = 0; t < tiles && ok; ++t) {
-                const uint32_t kv = k, kk = k + 1;
-                const bool last = t + 1 == tiles;
-                wait_stage(kv);
-                for (int i = 0; i < live && ok; ++i) {
-                    wait(kCbP + i, t & 1);
-                    if (!ok) break;
-                    tc_fence_after();
-                    if (i == 0) clear_padding(t, kv);
-                    output(i, kv, t > 0);
-                    if (i + 1 == live) release(kv);
-                    if (!last) {
-                        if (i == 0) wait_stage(kk);
-                        if (!ok) break;
-                        logits(i, kk);
-                        if (i + 1 == live) release(kk);
-                    } else if (leader) {
-                        tc_commit(bar(kCbO + i));
-                    }
-                    __syncwarp();
-                }
-                k += last ? 1 : 2;
+            if (leader && ok) {
+                release(at);
+                if (more) release(at + 1);
             }
+            __syncwarp();
         }
         if (any) {   // every product has finished before tensor memory is released
             if (leader) tc_commit(bar(kCbDrain));
@@ -287,13 +358,15 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
         __syncwarp();
     } else {
         // ---------------------------------------------------------------- softmax
-        const int i = S == 1 ? 0 : (warp - 2) >> 2, q = warp & 3, row = q * 32 + lane;   // (a warp may touch the TMEM lanes of its quarter)
-        const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16), ts = lanes + 128 * i, to = lanes + L::kOutCol + D * i;
+        const int i = (warp - 2) >> 3, half = ((warp - 2) >> 2) & 1, q = warp & 3, row = q * 32 + lane, pair = 1 + 4 * i + q;   // (a warp may touch the TMEM lanes of its quarter)
+        constexpr int W = L::kCols, W2 = D / 2;   // columns of S and O
+        const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16), ts = lanes + 128 * i + W * half, to = lanes + L::kOutCol + D * i + W2 * half;
         const int qt = kSplit ? 0 : i, ti = row / G, t = t0 + qt * p.tile_tokens + ti, g = row - ti * G;
         const bool valid = ti < tokens[qt], works = __any_sync(0xffffffffu, valid);
         const int mine = tiles <= 0 || tokens[qt] <= 0 ? 0 : kSplit ? (tiles - i + S - 1) / S : tiles;
         const float c = p.c.scale_log2e;
-        float m = -INFINITY, sum = 0.f;
+        float2 *stat = reinterpret_cast<float2 *>(ct_raw + L::kOffStat) + i * kCtRows + row;   // (what the row's two threads tell each other; at the end its statistics)
+        float m = -INFINITY, sum = 0.f;   // the sum is this half's
         for (int j = 0; j < mine; ++j) {
             const int tile = first + (kSplit ? j * S + i : j);
             // columns that this row sees
@@ -303,65 +376,22 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
             __syncwarp();
             tc_fence_after();
             if (works) {
-                uint32_t v[KT / 32][32];
+                bool general = j == 0 || masked;
+                if (!general) {
+                    uint32_t h[W / 32][16];
+                    const float s = chunk_tile<W>(ts, c, m, h);
+                    general = chunk_pair_any(pair, valid && !(s < kChunkMost));   // (the logits are still there)
+                    if (!general) {
+                        sum += s;
 #pragma unroll
-                for (int a = 0; a < KT / 32; ++a) tmem_ld32(ts + 32 * a, v[a]);
-#pragma unroll
-                for (int a = 0; a < KT / 32; ++a) tmem_wait_ld(v[a]);
-                if (masked) {
-#pragma unroll
-                    for (int a = 0; a < KT / 32; ++a)
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (32 * a + e >= cols) v[a][e] = __float_as_uint(-INFINITY);
-                }
-                float mx[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) mx[e] = max3(__uint_as_float(v[0][e]), __uint_as_float(v[0][e + 4]), __uint_as_float(v[0][e + 8]));
-#pragma unroll
-                for (int a = 0; a < KT / 32; ++a)
-#pragma unroll
-                    for (int e = a ? 0 : 12; e + 8 <= 32; e += 8)
-#pragma unroll
-                        for (int f = 0; f < 4; ++f) mx[f] = max3(mx[f], __uint_as_float(v[a][e + f]), __uint_as_float(v[a][e + f + 4]));
-#pragma unroll
-                for (int f = 0; f < 4; ++f) mx[f] = fmaxf(mx[f], __uint_as_float(v[0][28 + f]));
-                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * c;
-                const bool moves = valid && top > m + kChunkSlack;
-                if (__any_sync(0xffffffffu, moves)) {
-                    const float to_m = moves ? top : m, f = moves ? chunk_ex2(m - to_m) : 1.f;   // (m = -inf: 0)
-                    sum *= f;
-                    m = to_m;
-                    if (j > 0) {
-                        // the product that last added to O has finished: it was issued before the one that made this tile's logits
-#pragma unroll 1
-                        for (int a = 0; a < D / 32; ++a) {
-                            uint32_t o[32];
-                            tmem_ld32(to + 32 * a, o);
-                            tmem_wait_ld(o);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                            tmem_st32(to + 32 * a, o);
-                        }
+                        for (int a = 0; a < W / 32; ++a) tmem_st16(ts + 16 * a, h[a]);
                     }
                 }
-                const float ref = m == -INFINITY ? 0.f : m;
-                const float2 c2 = make_float2(c, c), r2 = make_float2(-ref, -ref);
-                float2 s2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-#pragma unroll
-                for (int a = 0; a < KT / 32; ++a)
-#pragma unroll
-                    for (int e = 0; e < 32; e += 2) {
-                        const float2 x = __ffma2_rn(make_float2(__uint_as_float(v[a][e]), __uint_as_float(v[a][e + 1])), c2, r2);
-                        const float2 w = make_float2(chunk_ex2(x.x), chunk_ex2(x.y));
-                        s2[(e >> 1) & 1] = __fadd2_rn(s2[(e >> 1) & 1], w);
-                        const __nv_bfloat162 h = __floats2bfloat162_rn(w.x, w.y);
-                        v[a >> 1][(a & 1) * 16 + (e >> 1)] = *reinterpret_cast<const uint32_t *>(&h);   // (two columns become one: what is overwritten has been used)
-                    }
-                const float2 s1 = __fadd2_rn(s2[0], s2[1]);
-                sum += s1.x + s1.y;
-#pragma unroll
-                for (int a = 0; a < KT / 64; ++a) tmem_st32(ts + 32 * a, v[a]);
+                if (general) {
+                    const float2 r = chunk_tile_general<W, W2>(ts, to, cols - W * half, c, m, sum, valid, j > 0, stat, half, pair);
+                    m = r.x;
+                    sum = r.y;
+                }
                 tmem_wait_st();
             }
             tc_fence_before();
@@ -373,32 +403,33 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
             __syncwarp();
             tc_fence_after();
         }
-        if (!p.merge) {
-            if (works && mine > 0) {   // (mine > 0 is uniform over the stream)
-                const float inv = 1.f / sum;
-                __nv_bfloat16 *o = (__nv_bfloat16 *)p.c.out + l * p.c.os.layer + b * p.c.os.stream + (long long)(hkv * G + g) * p.c.os.head + (long long)t * p.c.os.token;
+        if (works) {   // the two halves' sums
+            (half ? stat->y : stat->x) = sum;
+            chunk_pair_sync(pair);
+            sum = stat->x + stat->y;
+            chunk_pair_sync(pair);
+            if (p.merge && !half) *stat = make_float2(m, sum);   // (-inf, 0 where no key has been seen)
+        }
+        if (!p.merge && works && mine > 0) {   // (mine > 0 is uniform over the stream)
+            const float inv = 1.f / sum;
+            __nv_bfloat16 *o = (__nv_bfloat16 *)p.c.out + l * p.c.os.layer + b * p.c.os.stream + (long long)(hkv * G + g) * p.c.os.head + (long long)t * p.c.os.token + W2 * half;
 #pragma unroll 1
-                for (int a = 0; a < D / 32; ++a) {
-                    uint32_t x[32];
-                    tmem_ld32(to + 32 * a, x);
-                    tmem_wait_ld(x);
+            for (int a = 0; a < W2; a += 32) {
+                uint32_t x[32];
+                tmem_ld32(to + a, x);
+                tmem_wait_ld(x);
 #pragma unroll
-                    for (int e = 0; e < 32; e += 8) {
-                        uint32_t w[4];
+                for (int e = 0; e < 32; e += 8) {
+                    uint32_t w[4];
 #pragma unroll
-                        for (int f = 0; f < 4; ++f) {
-                            const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(x[e + 2 * f]) * inv, __uint_as_float(x[e + 2 * f + 1]) * inv);
-                            w[f] = *reinterpret_cast<const uint32_t *>(&h);
-                        }
-                        if (valid && 32 * a + e < p.c.d) *reinterpret_cast<uint4 *>(o + 32 * a + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                    for (int f = 0; f < 4; ++f) {
+                        const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(x[e + 2 * f]) * inv, __uint_as_float(x[e + 2 * f + 1]) * inv);
+                        w[f] = *reinterpret_cast<const uint32_t *>(&h);
                     }
+                    if (valid && W2 * half + a + e < p.c.d) *reinterpret_cast<uint4 *>(o + a + e) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
-                if (valid && p.c.lse) p.c.lse[(((size_t)l * p.c.streams + b) * p.c.Hkv * G + hkv * G + g) * p.c.n + t] = 0.6931471805599453f * (m + log2f(sum));
             }
-        } else if (works) {
-            // this stream's result into shared memory (the stages have been read: every product of this stream, and with it every key tile
-            // that it waits for, is done; the other stream's are in the way only after its own wait, hence the barrier below)
-            reinterpret_cast<float2 *>(ct_raw + L::kOffStat)[i * kCtRows + row] = make_float2(m, sum);
+            if (valid && !half && p.c.lse) p.c.lse[(((size_t)l * p.c.streams + b) * p.c.Hkv * G + hkv * G + g) * p.c.n + t] = 0.6931471805599453f * (m + log2f(sum));
         }
     }
     if (p.merge) {
@@ -408,14 +439,14 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
         float *part = reinterpret_cast<float *>(ct_raw + L::kOffStage);
         float2 *stat = reinterpret_cast<float2 *>(ct_raw + L::kOffStat);
         if (warp >= 2) {
-            const int i = S == 1 ? 0 : (warp - 2) >> 2, q = warp & 3, row = q * 32 + lane, qt = kSplit ? 0 : i;
+            const int i = (warp - 2) >> 3, half = ((warp - 2) >> 2) & 1, q = warp & 3, row = q * 32 + lane, qt = kSplit ? 0 : i;
             const bool works = __any_sync(0xffffffffu, row / G < tokens[qt]);
             const int mine = tiles <= 0 ? 0 : kSplit ? (tiles - i + S - 1) / S : tiles;
             if (works && mine > 0) {
-                const uint32_t to = tmem + ((uint32_t)(q * 32) << 16) + L::kOutCol + D * i;
-                float4 *dst = reinterpret_cast<float4 *>(part + (size_t)(i * kCtRows + row) * L::kPitch);
+                const uint32_t to = tmem + ((uint32_t)(q * 32) << 16) + L::kOutCol + D * i + D / 2 * half;
+                float4 *dst = reinterpret_cast<float4 *>(part + (size_t)(i * kCtRows + row) * L::kPitch + D / 2 * half);
 #pragma unroll 1
-                for (int a = 0; a < D / 32; ++a) {
+                for (int a = 0; a < D / 64; ++a) {
                     uint32_t x[32];
                     tmem_ld32(to + 32 * a, x);
                     tmem_wait_ld(x);
@@ -423,8 +454,6 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                     for (int e = 0; e < 8; ++e)
                         dst[a * 8 + e] = make_float4(__uint_as_float(x[4 * e]), __uint_as_float(x[4 * e + 1]), __uint_as_float(x[4 * e + 2]), __uint_as_float(x[4 * e + 3]));
                 }
-            } else if (works) {
-                stat[i * kCtRows + row] = make_float2(-INFINITY, 0.f);
             }
         }
         cluster_sync();
