@@ -123,15 +123,20 @@ __device__ __forceinline__ bool chunk_pair_any(int id, bool x)
 template <int W, int W2>
 __device__ __noinline__ float2 chunk_tile_general(uint32_t ts, uint32_t to, int cols, float c, float m, float sum, bool valid, bool scale, float2 *seen, int half, int pair)
 {
-    float top = -INFINITY;
-#pragma unroll 1
-    for (int a = 0; a < W; a += 32) {
-        uint32_t v[32];
-        tmem_ld32(ts + a, v);
-        tmem_wait_ld(v);
+    uint32_t v[W / 32][32];
+    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int e = 0; e < 32; ++e) top = fmaxf(top, a + e < cols ? __uint_as_float(v[e]) : -INFINITY);
+    for (int a = 0; a < W / 32; ++a) tmem_ld32(ts + 32 * a, v[a]);
+#pragma unroll
+    for (int a = 0; a < W / 32; ++a) {
+        tmem_wait_ld(v[a]);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+            if (32 * a + e >= cols) v[a][e] = __float_as_uint(-INFINITY);
+            mx[e & 3] = fmaxf(mx[e & 3], __uint_as_float(v[a][e]));
+        }
     }
+    float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
     (half ? seen->y : seen->x) = top;
     chunk_pair_sync(pair);
     top = fmaxf(seen->x, seen->y) * c;
@@ -155,20 +160,18 @@ __device__ __noinline__ float2 chunk_tile_general(uint32_t ts, uint32_t to, int 
     }
     const float ref = m == -INFINITY ? 0.f : m;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-    for (int a = 0; a < W; a += 32) {   // (what is stored lies in columns that have been read)
-        uint32_t v[32], h[16];
-        tmem_ld32(ts + a, v);
-        tmem_wait_ld(v);
+#pragma unroll
+    for (int a = 0; a < W / 32; ++a) {
+        uint32_t h[16];
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
-            const float x = a + e < cols ? chunk_ex2(fmaf(__uint_as_float(v[e]), c, -ref)) : 0.f, y = a + e + 1 < cols ? chunk_ex2(fmaf(__uint_as_float(v[e + 1]), c, -ref)) : 0.f;
+            const float x = chunk_ex2(fmaf(__uint_as_float(v[a][e]), c, -ref)), y = chunk_ex2(fmaf(__uint_as_float(v[a][e + 1]), c, -ref));   // (-inf: 0)
             s[e & 2] += x;
             s[(e & 2) + 1] += y;
             const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
             h[e >> 1] = *reinterpret_cast<const uint32_t *>(&b);
         }
-        tmem_st16(ts + (a >> 1), h);
+        tmem_st16(ts + 16 * a, h);
     }
     return make_float2(m, sum + ((s[0] + s[1]) + (s[2] + s[3])));
 }
@@ -456,9 +459,11 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                 }
             }
         }
-        cluster_sync();
+        if (ranks > 1) cluster_sync();
+        else __syncthreads();
         // a thread has 8 channels of a row; partial results of the cluster's blocks and, where the streams share a query tile, of both streams
-        const int vecs = p.c.d / 8, parts = kSplit ? S : 1;
+        const int vecs = p.c.d / 8;
+        constexpr int parts = kSplit ? S : 1;
         for (int qt = 0; qt < L::kQTiles; ++qt) {
             const int rows = max(tokens[qt], 0) * G;
             for (int e = rank * L::kThreads + threadIdx.x; e < rows * vecs; e += ranks * L::kThreads) {
@@ -467,16 +472,18 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
 #pragma unroll
                 for (int f = 0; f < 8; ++f) o[f] = 0.f;
                 for (uint32_t r = 0; r < ranks; ++r)
-                    for (int i = 0; i < parts; ++i) ref = fmaxf(ref, cluster_ld(cluster_addr(&stat[(qt + i) * kCtRows + row].x, r)));
-                for (uint32_t r = 0; r < ranks; ++r)
-                    for (int i = 0; i < parts; ++i) {
-                        const uint32_t st = cluster_addr(&stat[(qt + i) * kCtRows + row], r), src = cluster_addr(part + (size_t)((qt + i) * kCtRows + row) * L::kPitch + 8 * v, r);
-                        const float mr = cluster_ld(st);
-                        if (mr == -INFINITY) continue;   // it has seen no key of this row: what it holds is not a number
-                        const float f = chunk_ex2(mr - ref);
-                        den = fmaf(cluster_ld(st + 4), f, den);
 #pragma unroll
-                        for (int x = 0; x < 8; ++x) o[x] = fmaf(cluster_ld(src + 4 * x), f, o[x]);
+                    for (int i = 0; i < parts; ++i) {
+                        const float2 st = cluster_ld2(cluster_addr(&stat[(qt + i) * kCtRows + row], r));
+                        const uint32_t src = cluster_addr(part + (size_t)((qt + i) * kCtRows + row) * L::kPitch + 8 * v, r);
+                        const float4 x = cluster_ld4(src), y = cluster_ld4(src + 16);
+                        if (st.x == -INFINITY) continue;   // it has seen no key of this row: what it holds is not a number
+                        const float top = fmaxf(ref, st.x), f0 = chunk_ex2(ref - top), f = chunk_ex2(st.x - top);   // (ref = -inf: 0)
+                        ref = top;
+                        den = den * f0 + st.y * f;
+                        const float z[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+                        for (int e2 = 0; e2 < 8; ++e2) o[e2] = o[e2] * f0 + z[e2] * f;
                     }
                 const float inv = 1.f / den;
                 uint32_t w[4];
@@ -491,7 +498,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                 if (v == 0 && p.c.lse) p.c.lse[(((size_t)l * p.c.streams + b) * p.c.Hkv * G + hkv * G + g) * p.c.n + t] = 0.6931471805599453f * (ref + log2f(den));
             }
         }
-        cluster_sync();   // no block ends while others read its results
+        if (ranks > 1) cluster_sync();   // no block ends while others read its results
     }
     tc_fence_before();
     __syncthreads();
