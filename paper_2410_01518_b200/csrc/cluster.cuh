@@ -1,5 +1,7 @@
 // Thread-block clusters: their blocks' shared memory, and launches.
 #pragma once
+#include <atomic>
+
 #include "common.cuh"
 
 namespace ipotk {
@@ -64,20 +66,11 @@ __device__ __forceinline__ void cluster_st(uint32_t addr, float4 v)
 __device__ __forceinline__ void cluster_st(uint32_t addr, float2 v) { asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(addr), "f"(v.x), "f"(v.y) : "memory"); }
 __device__ __forceinline__ void cluster_st(uint32_t addr, double v) { asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(addr), "d"(v) : "memory"); }
 
-// A launch of clusters along x (more than 8 blocks are not portable, but this part has 16), as a programmatic dependent like launch_pdl's.
-template <typename... P, typename... A>
-inline cudaError_t launch_cluster(void (*kern)(P...), dim3 grid, dim3 block, size_t smem, int cluster, cudaStream_t stream, const A &...args)
+inline void cluster_config(cudaLaunchConfig_t &lc, cudaLaunchAttribute (&at)[2], dim3 grid, dim3 block, size_t smem, int cluster)
 {
-    if (cluster > 8) {
-        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-        if (e != cudaSuccess) return e;
-    }
-    cudaLaunchConfig_t lc = {};
     lc.gridDim = grid;
     lc.blockDim = block;
     lc.dynamicSmemBytes = smem;
-    lc.stream = stream;
-    cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = cluster;
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
@@ -85,7 +78,44 @@ inline cudaError_t launch_cluster(void (*kern)(P...), dim3 grid, dim3 block, siz
     at[1].val.programmaticStreamSerializationAllowed = 1;
     lc.attrs = at;
     lc.numAttrs = 2;
+}
+
+// A launch of clusters along x, as a programmatic dependent like launch_pdl's.
+template <typename... P, typename... A>
+inline cudaError_t launch_cluster(void (*kern)(P...), dim3 grid, dim3 block, size_t smem, int cluster, cudaStream_t stream, const A &...args)
+{
+    cudaLaunchConfig_t lc = {};
+    cudaLaunchAttribute at[2];
+    cluster_config(lc, at, grid, block, smem, cluster);
+    lc.stream = stream;
     return cudaLaunchKernelEx(&lc, kern, P(args)...);
+}
+
+// Blocks of a cluster for `items` pieces of work, each spread over one: the most, up to `most`, with which all clusters run side by side.  How many do is the driver's answer, asked once
+// per kernel and size: the blocks of a cluster share a GPC, and with one block an SM 15 clusters of 8 fit this part, not 18.  (More than 8 blocks are not portable, but it has 16.)
+constexpr int kMostRanks = 16;
+struct ClusterFit {
+    std::atomic<int> fits[kMostRanks + 1];   // 0: not asked yet
+};
+template <typename Kernel>
+inline int choose_cluster(ClusterFit &fit, Kernel kern, dim3 block, size_t smem, long long items, int most)
+{
+    for (int c = most < kMostRanks ? most : kMostRanks; c > 1; --c) {
+        int n = fit.fits[c].load(std::memory_order_relaxed);
+        if (!n) {
+            cudaLaunchConfig_t lc = {};
+            cudaLaunchAttribute at[2];
+            cluster_config(lc, at, dim3(c), block, smem, c);
+            if ((c > 8 && cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) || cudaOccupancyMaxActiveClusters(&n, kern, &lc) != cudaSuccess) {
+                cudaGetLastError();
+                n = 0;
+            }
+            if (n < 1) n = -1;   // (none)
+            fit.fits[c].store(n, std::memory_order_relaxed);
+        }
+        if (items <= n) return c;
+    }
+    return 1;
 }
 
 }  // namespace ipotk

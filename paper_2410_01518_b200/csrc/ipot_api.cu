@@ -1243,7 +1243,7 @@ int ipot_decode_attention_blocks(ipot_t *p, int layer, int n_layers, const void 
     b.unit_rows = p->cfg.pot_size; b.unit_blocks = p->blk_count; b.len = p->len; b.block_rows = p->blk_rows; b.blocks = n_blocks;
     b.n = 1; b.layers = n_layers; b.streams = p->cfg.batch; b.Hkv = p->cfg.Hkv; b.G = p->G; b.d = p->cfg.d;
     b.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)p->cfg.d));
-    IPOT_CUDA(launch_decode_blocks(b, p->cfg.dtype == IPOT_F32, p->sm_count, p->stream));
+    IPOT_CUDA(launch_decode_blocks(b, p->cfg.dtype == IPOT_F32, p->stream));
     p->launches += 1;
     return IPOT_OK;
 }

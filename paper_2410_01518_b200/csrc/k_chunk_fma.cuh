@@ -7,6 +7,8 @@
 // d / 16 channels of O += P V in registers; P goes through shared memory.  Few row tiles spread their keys over a cluster, whose blocks merge through distributed shared
 // memory.  Bound: FMA issue and shared-memory reads (32 packed FMAs per eight 16-byte reads).
 #pragma once
+#include <algorithm>
+
 #include "common.cuh"
 #include "ops.h"
 #include "cluster.cuh"
@@ -227,7 +229,7 @@ chunk_fma_kernel(const __grid_constant__ ChunkParams p, int units)
 }
 
 template <typename T, int DP>
-inline cudaError_t launch_chunk_fma_t(const ChunkParams &p, int sm_count, cudaStream_t stream)
+inline cudaError_t launch_chunk_fma_t(const ChunkParams &p, cudaStream_t stream)
 {
     const size_t smem = sizeof(ChunkFmaSmem<DP>);
     auto kern = chunk_fma_kernel<T, DP>;
@@ -235,17 +237,16 @@ inline cudaError_t launch_chunk_fma_t(const ChunkParams &p, int sm_count, cudaSt
     if (e != cudaSuccess) return e;
     const int units = p.layers * p.streams * p.Hkv;
     const long long items = ((long long)p.n * p.G + kCfRows - 1) / kCfRows * units;
-    // blocks of a cluster: as many as SMs are left for, with two key tiles each
-    int cluster = 1;
-    while (cluster < 8 && items * cluster * 2 <= sm_count && p.len + p.n > 4 * cluster * kCfKeys) cluster *= 2;
+    static ClusterFit fit;
+    const int cluster = choose_cluster(fit, kern, dim3(kCfThreads), smem, items, std::min(8, (p.len + p.n + 2 * kCfKeys - 1) / (2 * kCfKeys)));   // two key tiles each
     if (items * cluster > 0x7fffffff) return cudaErrorInvalidValue;
     return launch_cluster(kern, dim3((unsigned)(items * cluster)), dim3(kCfThreads), smem, cluster, stream, p, units);
 }
 
 template <typename T>
-inline cudaError_t launch_chunk_fma(const ChunkParams &p, int sm_count, cudaStream_t stream)
+inline cudaError_t launch_chunk_fma(const ChunkParams &p, cudaStream_t stream)
 {
-    return p.d <= 64 ? launch_chunk_fma_t<T, 64>(p, sm_count, stream) : p.d <= 128 ? launch_chunk_fma_t<T, 128>(p, sm_count, stream) : launch_chunk_fma_t<T, 256>(p, sm_count, stream);
+    return p.d <= 64 ? launch_chunk_fma_t<T, 64>(p, stream) : p.d <= 128 ? launch_chunk_fma_t<T, 128>(p, stream) : launch_chunk_fma_t<T, 256>(p, stream);
 }
 
 }  // namespace ipotk

@@ -48,7 +48,7 @@ template <int D, bool kSplit> struct ChunkTc {
     static constexpr uint32_t kOutCol = 256;                                 // tensor memory: S of stream i at 128 i, O at 256 + D i
     static constexpr int kThreads = 64 + 256 * kStreams;
     static constexpr int kCols = kKeys / 2;                                  // of a softmax thread
-    static_assert(kStreams * kCtRows * kPitch * 4 <= kStages * kStageBytes, "partial results take the stages' place");
+    static_assert(kCtRows * kPitch * 4 <= kStages * kStageBytes, "partial results take the stages' place");
     static_assert(kSmemBytes <= 232448, "shared memory of a block");
 };
 enum { kCbQ = 0, kCbFull = 1, kCbEmpty = 9, kCbS = 17, kCbP = 19, kCbO = 21, kCbDrain = 23, kCbCount = 24 };
@@ -411,9 +411,9 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
             chunk_pair_sync(pair);
             sum = stat->x + stat->y;
             chunk_pair_sync(pair);
-            if (p.merge && !half) *stat = make_float2(m, sum);   // (-inf, 0 where no key has been seen)
+            if (kSplit && !half) *stat = make_float2(m, sum);   // (-inf, 0 where no key has been seen)
         }
-        if (!p.merge && works && mine > 0) {   // (mine > 0 is uniform over the stream)
+        if (!kSplit && works && mine > 0) {   // (mine > 0 is uniform over the stream)
             const float inv = 1.f / sum;
             __nv_bfloat16 *o = (__nv_bfloat16 *)p.c.out + l * p.c.os.layer + b * p.c.os.stream + (long long)(hkv * G + g) * p.c.os.head + (long long)t * p.c.os.token + W2 * half;
 #pragma unroll 1
@@ -435,70 +435,120 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
             if (valid && !half && p.c.lse) p.c.lse[(((size_t)l * p.c.streams + b) * p.c.Hkv * G + hkv * G + g) * p.c.n + t] = 0.6931471805599453f * (m + log2f(sum));
         }
     }
-    if (p.merge) {
+    if (kSplit) {
+        // ---- the streams' results become one, and the cluster's blocks'
         tc_fence_before();
         __syncthreads();   // all products are done: the stages' memory is free
         tc_fence_after();
-        float *part = reinterpret_cast<float *>(ct_raw + L::kOffStage);
+        float *part = reinterpret_cast<float *>(ct_raw + L::kOffStage);   // [128][pitch]
         float2 *stat = reinterpret_cast<float2 *>(ct_raw + L::kOffStat);
-        if (warp >= 2) {
-            const int i = (warp - 2) >> 3, half = ((warp - 2) >> 2) & 1, q = warp & 3, row = q * 32 + lane, qt = kSplit ? 0 : i;
-            const bool works = __any_sync(0xffffffffu, row / G < tokens[qt]);
-            const int mine = tiles <= 0 ? 0 : kSplit ? (tiles - i + S - 1) / S : tiles;
-            if (works && mine > 0) {
-                const uint32_t to = tmem + ((uint32_t)(q * 32) << 16) + L::kOutCol + D * i + D / 2 * half;
-                float4 *dst = reinterpret_cast<float4 *>(part + (size_t)(i * kCtRows + row) * L::kPitch + D / 2 * half);
+        const int i = warp < 2 ? -1 : (warp - 2) >> 3, half = ((warp - 2) >> 2) & 1, q = warp & 3, row = q * 32 + lane;
+        const int ti = row / G, t = t0 + ti, g = row - ti * G;
+        const bool valid = ti < tokens[0], works = __any_sync(0xffffffffu, valid), mine0 = tiles > 0, mine1 = S == 2 && tiles > 1;   // (which streams have had keys)
+        const float2 s0 = stat[row], s1 = S == 2 ? stat[(S - 1) * kCtRows + row] : make_float2(-INFINITY, 0.f);
+        const float ref = fmaxf(s0.x, s1.x), f0 = s0.x == -INFINITY ? 0.f : chunk_ex2(s0.x - ref), f1 = s1.x == -INFINITY ? 0.f : chunk_ex2(s1.x - ref), den = s0.y * f0 + s1.y * f1;
+        float4 *at = reinterpret_cast<float4 *>(part + (size_t)row * L::kPitch + D / 2 * half);
+        const uint32_t to = tmem + ((uint32_t)(q * 32) << 16) + L::kOutCol + D / 2 * half;
+        if (i == 1 && works && mine1) {
 #pragma unroll 1
-                for (int a = 0; a < D / 64; ++a) {
-                    uint32_t x[32];
-                    tmem_ld32(to + 32 * a, x);
-                    tmem_wait_ld(x);
+            for (int a = 0; a < D / 64; ++a) {
+                uint32_t x[32];
+                tmem_ld32(to + D + 32 * a, x);
+                tmem_wait_ld(x);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        dst[a * 8 + e] = make_float4(__uint_as_float(x[4 * e]), __uint_as_float(x[4 * e + 1]), __uint_as_float(x[4 * e + 2]), __uint_as_float(x[4 * e + 3]));
-                }
+                for (int e = 0; e < 8; ++e)
+                    at[a * 8 + e] = make_float4(__uint_as_float(x[4 * e]) * f1, __uint_as_float(x[4 * e + 1]) * f1, __uint_as_float(x[4 * e + 2]) * f1, __uint_as_float(x[4 * e + 3]) * f1);
             }
         }
-        if (ranks > 1) cluster_sync();
-        else __syncthreads();
-        // a thread has 8 channels of a row; partial results of the cluster's blocks and, where the streams share a query tile, of both streams
-        const int vecs = p.c.d / 8;
-        constexpr int parts = kSplit ? S : 1;
-        for (int qt = 0; qt < L::kQTiles; ++qt) {
-            const int rows = max(tokens[qt], 0) * G;
+        __syncthreads();
+        if (i == 0 && works) {
+            const float inv = 1.f / den;
+            __nv_bfloat16 *o = (__nv_bfloat16 *)p.c.out + l * p.c.os.layer + b * p.c.os.stream + (long long)(hkv * G + g) * p.c.os.head + (long long)t * p.c.os.token + D / 2 * half;
+#pragma unroll 1
+            for (int a = 0; a < D / 64; ++a) {
+                uint32_t x[32];
+                if (mine0) {
+                    tmem_ld32(to + 32 * a, x);
+                    tmem_wait_ld(x);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float4 y = mine1 ? at[a * 8 + e] : make_float4(0.f, 0.f, 0.f, 0.f);
+                    const float z[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) x[4 * e + k] = __float_as_uint(mine0 ? fmaf(__uint_as_float(x[4 * e + k]), f0, z[k]) : 0.f);
+                    if (ranks > 1) at[a * 8 + e] = make_float4(__uint_as_float(x[4 * e]), __uint_as_float(x[4 * e + 1]), __uint_as_float(x[4 * e + 2]), __uint_as_float(x[4 * e + 3]));
+                }
+                if (ranks == 1) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 8) {
+                        uint32_t w[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const __nv_bfloat162 h = __floats2bfloat162_rn(__uint_as_float(x[e + 2 * k]) * inv, __uint_as_float(x[e + 2 * k + 1]) * inv);
+                            w[k] = *reinterpret_cast<const uint32_t *>(&h);
+                        }
+                        if (valid && D / 2 * half + 32 * a + e < p.c.d) *reinterpret_cast<uint4 *>(o + 32 * a + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                    }
+                }
+            }
+            if (ranks > 1) {
+                if (!half) stat[row] = make_float2(ref, den);   // (everyone has read what was there)
+            } else if (valid && !half && p.c.lse) {
+                p.c.lse[(((size_t)l * p.c.streams + b) * p.c.Hkv * G + hkv * G + g) * p.c.n + t] = 0.6931471805599453f * (ref + log2f(den));
+            }
+        }
+        if (ranks > 1) {
+            cluster_sync();
+            // a thread has 8 channels of a row; four blocks' values of them on their way at once
+            const int vecs = p.c.d / 8, rows = max(tokens[0], 0) * G;
             for (int e = rank * L::kThreads + threadIdx.x; e < rows * vecs; e += ranks * L::kThreads) {
                 const int row = e / vecs, v = e - row * vecs;
                 float ref = -INFINITY, den = 0.f, o[8];
 #pragma unroll
-                for (int f = 0; f < 8; ++f) o[f] = 0.f;
-                for (uint32_t r = 0; r < ranks; ++r)
+                for (int k = 0; k < 8; ++k) o[k] = 0.f;
+                for (uint32_t r0 = 0; r0 < ranks; r0 += 4) {   // (1, 2, 4 or 8 blocks)
+                    float2 st[4];
+                    float4 x[4], y[4];
 #pragma unroll
-                    for (int i = 0; i < parts; ++i) {
-                        const float2 st = cluster_ld2(cluster_addr(&stat[(qt + i) * kCtRows + row], r));
-                        const uint32_t src = cluster_addr(part + (size_t)((qt + i) * kCtRows + row) * L::kPitch + 8 * v, r);
-                        const float4 x = cluster_ld4(src), y = cluster_ld4(src + 16);
-                        if (st.x == -INFINITY) continue;   // it has seen no key of this row: what it holds is not a number
-                        const float top = fmaxf(ref, st.x), f0 = chunk_ex2(ref - top), f = chunk_ex2(st.x - top);   // (ref = -inf: 0)
-                        ref = top;
-                        den = den * f0 + st.y * f;
-                        const float z[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
-#pragma unroll
-                        for (int e2 = 0; e2 < 8; ++e2) o[e2] = o[e2] * f0 + z[e2] * f;
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t r = min(r0 + k, ranks - 1), src = cluster_addr(part + (size_t)row * L::kPitch + 8 * v, r);
+                        st[k] = cluster_ld2(cluster_addr(&stat[row], r));
+                        x[k] = cluster_ld4(src);
+                        y[k] = cluster_ld4(src + 16);
+                        if (r0 + k >= ranks) st[k] = make_float2(-INFINITY, 0.f);
                     }
+                    float top = ref;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) top = fmaxf(top, st[k].x);
+                    const float fr = ref == -INFINITY ? 0.f : chunk_ex2(ref - top);
+                    ref = top;
+                    den *= fr;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) o[k] *= fr;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if (st[k].x == -INFINITY) continue;   // it has seen no key of this row: what it holds is not a number
+                        const float f = chunk_ex2(st[k].x - ref), z[8] = {x[k].x, x[k].y, x[k].z, x[k].w, y[k].x, y[k].y, y[k].z, y[k].w};
+                        den = fmaf(st[k].y, f, den);
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) o[c] = fmaf(z[c], f, o[c]);
+                    }
+                }
                 const float inv = 1.f / den;
                 uint32_t w[4];
 #pragma unroll
-                for (int f = 0; f < 4; ++f) {
-                    const __nv_bfloat162 h = __floats2bfloat162_rn(o[2 * f] * inv, o[2 * f + 1] * inv);
-                    w[f] = *reinterpret_cast<const uint32_t *>(&h);
+                for (int k = 0; k < 4; ++k) {
+                    const __nv_bfloat162 h = __floats2bfloat162_rn(o[2 * k] * inv, o[2 * k + 1] * inv);
+                    w[k] = *reinterpret_cast<const uint32_t *>(&h);
                 }
-                const int ti = row / G, g = row - ti * G, t = t0 + qt * p.tile_tokens + ti;
+                const int ti = row / G, g = row - ti * G, t = t0 + ti;
                 __nv_bfloat16 *out = (__nv_bfloat16 *)p.c.out + l * p.c.os.layer + b * p.c.os.stream + (long long)(hkv * G + g) * p.c.os.head + (long long)t * p.c.os.token;
                 *reinterpret_cast<uint4 *>(out + 8 * v) = make_uint4(w[0], w[1], w[2], w[3]);
                 if (v == 0 && p.c.lse) p.c.lse[(((size_t)l * p.c.streams + b) * p.c.Hkv * G + hkv * G + g) * p.c.n + t] = 0.6931471805599453f * (ref + log2f(den));
             }
+            cluster_sync();   // no block ends while others read its results
         }
-        if (ranks > 1) cluster_sync();   // no block ends while others read its results
     }
     tc_fence_before();
     __syncthreads();
@@ -531,7 +581,7 @@ inline bool chunk_pot_map(TcEncodeFn encode, CUtensorMap *map, const void *ptr, 
 
 // *done: the call has been launched (or failed to be); false: its strides are none that a tensor map takes.
 template <int D, bool kSplit>
-inline cudaError_t launch_chunk_tc_t(const ChunkParams &c, const ChunkTcHost &host, int tile_tokens, int tiles, int cluster, cudaStream_t stream, bool *done)
+inline cudaError_t launch_chunk_tc_t(const ChunkParams &c, const ChunkTcHost &host, int tile_tokens, int tiles, cudaStream_t stream, bool *done)
 {
     using L = ChunkTc<D, kSplit>;
     *done = false;
@@ -546,32 +596,35 @@ inline cudaError_t launch_chunk_tc_t(const ChunkParams &c, const ChunkTcHost &ho
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)L::kSmemBytes);
     if (e != cudaSuccess) return e;
     ChunkTcParams p;
+    const long long items = (long long)c.layers * c.streams * c.Hkv * ((tiles + L::kQTiles - 1) / L::kQTiles);
+    const int key_tiles = (c.len + L::kKeys - 1) / L::kKeys + (c.n + L::kKeys - 1) / L::kKeys;
+    static ClusterFit fit;
+    // few query tiles: a tile's keys over a cluster, two key tiles a block
+    const int cluster = kSplit ? choose_cluster(fit, kern, dim3(L::kThreads), L::kSmemBytes, items, std::min(8, (key_tiles + 1) / 2)) : 1;
+    if (items * cluster > 0x7fffffff) return cudaErrorInvalidValue;
     p.c = c;
     p.tile_tokens = tile_tokens;
     p.items_per_unit = (tiles + L::kQTiles - 1) / L::kQTiles;
-    p.merge = kSplit || cluster > 1;
     p.withhold = host.withhold;
     p.wait_ns = host.wait_ns;
     p.status = c.status;
-    return launch_cluster(kern, dim3((unsigned)cluster * p.items_per_unit * (unsigned)(c.layers * c.streams * c.Hkv)), dim3(L::kThreads), L::kSmemBytes, cluster, stream, q, K, V, k, v, p);
+    return launch_cluster(kern, dim3((unsigned)(cluster * items)), dim3(L::kThreads), L::kSmemBytes, cluster, stream, q, K, V, k, v, p);
 }
 
 inline cudaError_t launch_chunk_tc(const ChunkParams &c, const ChunkTcHost &host, cudaStream_t stream, bool *done)
 {
     const int tile_tokens = kCtRows / c.G, tiles = (c.n + tile_tokens - 1) / tile_tokens;
     const long long units = (long long)c.layers * c.streams * c.Hkv;
-    // two query tiles a block share its key tiles where that leaves no SM without work
-    const bool pairs = c.d <= 128 && units * ((tiles + 1) / 2) >= host.sm_count;
-    const long long items = units * (pairs ? (tiles + 1) / 2 : tiles);
-    const int keys = c.d > 128 ? 64 : 128, key_tiles = (c.len + keys - 1) / keys + (c.n + keys - 1) / keys;
-    int cluster = 1;
-    while (!pairs && cluster < 8 && items * cluster * 2 <= host.sm_count && key_tiles >= 4 * cluster) cluster *= 2;
-    if (items * cluster > 0x7fffffff) return cudaErrorInvalidValue;
-    if (c.d > 128) return launch_chunk_tc_t<256, true>(c, host, tile_tokens, tiles, cluster, stream, done);
-    if (c.d > 64) return pairs ? launch_chunk_tc_t<128, false>(c, host, tile_tokens, tiles, cluster, stream, done)
-                               : launch_chunk_tc_t<128, true>(c, host, tile_tokens, tiles, cluster, stream, done);
-    return pairs ? launch_chunk_tc_t<64, false>(c, host, tile_tokens, tiles, cluster, stream, done)
-                 : launch_chunk_tc_t<64, true>(c, host, tile_tokens, tiles, cluster, stream, done);
+    // Two query tiles a block share its key tiles where one tile a block would need more than a round of blocks (us, two / one: 2 x 3 streams x 333 tokens over 1999 rows, 4 KV
+    // heads 44 / 53; 1024 over 2048, 8 KV heads 53 / 61; 2 x 512 over 4096 74 / 90).  Streams of different lengths: how long the host does not know; a quarter of the tiles
+    // is taken to be padding (the first of these with 333, 222 and 111 tokens: 43 / 30).
+    const long long all = units * tiles;
+    const bool pairs = c.d <= 128 && (c.tokens ? all - all / 4 : all) > host.sm_count;
+    if (c.d > 128) return launch_chunk_tc_t<256, true>(c, host, tile_tokens, tiles, stream, done);
+    if (c.d > 64) return pairs ? launch_chunk_tc_t<128, false>(c, host, tile_tokens, tiles, stream, done)
+                               : launch_chunk_tc_t<128, true>(c, host, tile_tokens, tiles, stream, done);
+    return pairs ? launch_chunk_tc_t<64, false>(c, host, tile_tokens, tiles, stream, done)
+                 : launch_chunk_tc_t<64, true>(c, host, tile_tokens, tiles, stream, done);
 }
 
 }  // namespace ipotk

@@ -33,7 +33,7 @@ __device__ __forceinline__ float few_ex2(float x)
 // 2^(m - ref), 0 where nothing has been seen (m = -inf) whatever ref is
 __device__ __forceinline__ float few_scale(float m, float ref) { return m == -INFINITY ? 0.f : few_ex2(m - ref); }
 
-constexpr int kFewThreads = 128, kFewWarps = kFewThreads / 32, kFewMaxRanks = 16;
+constexpr int kFewThreads = 128, kFewWarps = kFewThreads / 32, kFewMaxRanks = kMostRanks;
 constexpr int kFewRows = 8;       // query rows of a block
 constexpr int kFewBlocks = 2048;  // blocks of a unit: 32768 slots, 16 rows
 constexpr int kScoreBytes = kFewBlocks * (int)sizeof(double);
@@ -782,52 +782,54 @@ few_fma_kernel(const __grid_constant__ FewParams p, int lpk)
 }
 
 // ------------------------------------------------------------------ host side
+// blocks of a cluster: as many as find a place at once, and at least one tile of 16 keys for every warp.  (8 warps a block, one on an SM: a cluster of 16 then needs 16 SMs of one
+// GPC to itself, and 8 of them do not run side by side: one token over 4095 rows, 8 units 13.8 us against 8.9.)
 template <typename... A>
-inline cudaError_t launch_few_t(void (*kern)(FewParams, A...), const FewParams &p, size_t smem, int cluster, cudaStream_t stream, A... args)
+inline cudaError_t launch_few_t(ClusterFit &fit, void (*kern)(FewParams, A...), const FewParams &p, size_t smem, int keys, cudaStream_t stream, A... args)
 {
     const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
     if (e != cudaSuccess) return e;
-    return launch_cluster(kern, dim3(cluster, p.layers * p.streams * p.Hkv, (p.n * p.G + kFewRows - 1) / kFewRows), dim3(kFewThreads), smem, cluster, stream, p, args...);
+    const dim3 block(kFewThreads);
+    const int groups = (p.n * p.G + kFewRows - 1) / kFewRows, units = p.layers * p.streams * p.Hkv;
+    const int cluster = choose_cluster(fit, kern, block, smem, (long long)units * groups, (keys + 16 * kFewWarps - 1) / (16 * kFewWarps));
+    return launch_cluster(kern, dim3(cluster, units, groups), block, smem, cluster, stream, p, args...);
 }
 
 template <int R, int VPL, bool kSparse>
-inline cudaError_t launch_few_fma(const FewParams &p, int lpk, int cluster, cudaStream_t stream)
+inline cudaError_t launch_few_fma(const FewParams &p, int lpk, int keys, cudaStream_t stream)
 {
+    static ClusterFit fit;
     size_t part = (size_t)kFewWarps * R * (p.d + 4) * sizeof(float);
     if (kSparse && part < kScoreBytes + kFewFmaRoom) part = kScoreBytes + kFewFmaRoom;
-    return launch_few_t<int>(few_fma_kernel<R, VPL, kSparse>, p, sizeof(FewShared) + (R * p.d + 4 * kFewMaxRanks) * sizeof(float) + part, cluster, stream, lpk);
+    return launch_few_t<int>(fit, few_fma_kernel<R, VPL, kSparse>, p, sizeof(FewShared) + (R * p.d + 4 * kFewMaxRanks) * sizeof(float) + part, keys, stream, lpk);
 }
 
 template <int D, bool kSparse>
-inline cudaError_t launch_few_mma(const FewParams &p, int cluster, cudaStream_t stream)
+inline cudaError_t launch_few_mma(const FewParams &p, int keys, cudaStream_t stream)
 {
+    static ClusterFit fit;
     using Ring = FewRing<D>;
-    return launch_few_t<>(few_mma_kernel<D, kSparse>, p, Ring::kBytes + sizeof(FewShared) + Ring::kGot, cluster, stream);
+    return launch_few_t<>(fit, few_mma_kernel<D, kSparse>, p, Ring::kBytes + sizeof(FewShared) + Ring::kGot, keys, stream);
 }
 
 template <bool kSparse>
-inline cudaError_t launch_few(const FewParams &p, bool f32, int sm_count, cudaStream_t stream)
+inline cudaError_t launch_few(const FewParams &p, bool f32, cudaStream_t stream)
 {
-    // blocks of a cluster: as many as find a place at once (two on an SM), and at least one tile of 16 keys for every warp.  (8 warps a block, one on an
-    // SM: a cluster of 16 then needs 16 SMs of one GPC to itself, and 8 of them do not run side by side: one token over 4095 rows, 8 units 13.8 us against 8.9.)
-    const long long units = (long long)p.layers * p.streams * p.Hkv * ((p.n * p.G + kFewRows - 1) / kFewRows);
     const int keys = kSparse ? (p.len < p.blocks * p.block_rows ? p.len : p.blocks * p.block_rows) : p.len + p.n;
-    int cluster = 1;
-    while (cluster < kFewMaxRanks && units * cluster * 2 <= 2LL * sm_count && keys > cluster * 16 * kFewWarps) cluster *= 2;
     if (!f32) {
-        if (p.d <= 64) return launch_few_mma<64, kSparse>(p, cluster, stream);
-        return p.d <= 128 ? launch_few_mma<128, kSparse>(p, cluster, stream) : launch_few_mma<256, kSparse>(p, cluster, stream);
+        if (p.d <= 64) return launch_few_mma<64, kSparse>(p, keys, stream);
+        return p.d <= 128 ? launch_few_mma<128, kSparse>(p, keys, stream) : launch_few_mma<256, kSparse>(p, keys, stream);
     }
     const int vecs = p.d / 4, rows = p.n * p.G;
     int lpk = 1;
     while (lpk < vecs && lpk < 32) lpk *= 2;
     if (vecs > 32) {
-        if (rows == 1) return launch_few_fma<1, 2, kSparse>(p, lpk, cluster, stream);
-        return rows <= 4 ? launch_few_fma<4, 2, kSparse>(p, lpk, cluster, stream) : launch_few_fma<8, 2, kSparse>(p, lpk, cluster, stream);
+        if (rows == 1) return launch_few_fma<1, 2, kSparse>(p, lpk, keys, stream);
+        return rows <= 4 ? launch_few_fma<4, 2, kSparse>(p, lpk, keys, stream) : launch_few_fma<8, 2, kSparse>(p, lpk, keys, stream);
     }
-    if (rows == 1) return launch_few_fma<1, 1, kSparse>(p, lpk, cluster, stream);
-    if (rows == 2) return launch_few_fma<2, 1, kSparse>(p, lpk, cluster, stream);
-    return rows <= 4 ? launch_few_fma<4, 1, kSparse>(p, lpk, cluster, stream) : launch_few_fma<8, 1, kSparse>(p, lpk, cluster, stream);
+    if (rows == 1) return launch_few_fma<1, 1, kSparse>(p, lpk, keys, stream);
+    if (rows == 2) return launch_few_fma<2, 1, kSparse>(p, lpk, keys, stream);
+    return rows <= 4 ? launch_few_fma<4, 1, kSparse>(p, lpk, keys, stream) : launch_few_fma<8, 1, kSparse>(p, lpk, keys, stream);
 }
 
 }  // namespace ipotk

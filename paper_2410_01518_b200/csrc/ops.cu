@@ -39,9 +39,9 @@ cudaError_t launch_chunk_attention(const ChunkParams &p, bool f32, const ChunkTc
         f.out = p.out; f.os = p.os; f.lse = p.lse;
         f.layers = p.layers; f.streams = p.streams; f.Hkv = p.Hkv; f.G = p.G; f.d = p.d;
         f.scale_log2e = p.scale_log2e;
-        return launch_few<false>(f, f32, host.sm_count, stream);
+        return launch_few<false>(f, f32, stream);
     }
-    if (f32) return launch_chunk_fma<float>(p, host.sm_count, stream);
+    if (f32) return launch_chunk_fma<float>(p, stream);
     if (host.encode && p.G <= kCtRows) {
         bool done = false;
         ChunkParams t = p;
@@ -49,7 +49,7 @@ cudaError_t launch_chunk_attention(const ChunkParams &p, bool f32, const ChunkTc
         const cudaError_t e = launch_chunk_tc(t, host, stream, &done);
         if (done || e != cudaSuccess) return e;
     }
-    return launch_chunk_fma<__nv_bfloat16>(p, host.sm_count, stream);
+    return launch_chunk_fma<__nv_bfloat16>(p, stream);
 }
 
 cudaError_t launch_block_bounds(const void *K, void *lo, void *hi, int first_row, int len, int rows, int d, int units, size_t unit_rows, int unit_blocks, bool f32,
@@ -66,9 +66,9 @@ cudaError_t launch_append_bounds(const void *srcK, const void *srcV, void *potK,
                : launch_append_bounds_t<__nv_bfloat16>(srcK, srcV, potK, potV, lo, hi, first_row, n, rows, d, units, unit_rows, unit_blocks, sm_count, stream);
 }
 
-cudaError_t launch_decode_blocks(const FewParams &p, bool f32, int sm_count, cudaStream_t stream)
+cudaError_t launch_decode_blocks(const FewParams &p, bool f32, cudaStream_t stream)
 {
-    return launch_few<true>(p, f32, sm_count, stream);
+    return launch_few<true>(p, f32, stream);
 }
 
 }  // namespace ipotk

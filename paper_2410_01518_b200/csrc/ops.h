@@ -60,7 +60,6 @@ struct ChunkTcHost {
 struct ChunkTcParams {
     ChunkParams c;
     int tile_tokens, items_per_unit;
-    bool merge;
     int withhold;
     unsigned long long wait_ns;
     int *status;
@@ -88,7 +87,7 @@ struct FewParams {
     int layers, streams, Hkv, G, d;
     float scale_log2e;
 };
-cudaError_t launch_decode_blocks(const FewParams &p, bool f32, int sm_count, cudaStream_t stream);
+cudaError_t launch_decode_blocks(const FewParams &p, bool f32, cudaStream_t stream);
 // bounds of the blocks that hold rows [first_row, len) of every unit
 cudaError_t launch_block_bounds(const void *K, void *lo, void *hi, int first_row, int len, int rows, int d, int units, size_t unit_rows, int unit_blocks, bool f32,
                                 cudaStream_t stream);
