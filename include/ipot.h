@@ -128,11 +128,13 @@ int ipot_set_scorer(ipot_t *pot, int scorer);
  *   IPOT_TUNE_WAIT_LIMIT_NS       time after which a device-side wait of a tensor-core scorer gives up and the launch
  *                                 ends with IPOT_E_TIMEOUT in the status word (default 200 ms; at least 1000).
  *                                 The two-sweep scorers count it from the start of each wait, IPOT_SCORER_TENSOR
- *                                 from the start of each thread block (a launch of either takes well under 1 ms)
+ *                                 from the start of each thread block (a launch of either takes well under 1 ms).
+ *                                 The same limit holds for each wait of ipot_chunk_attention in bf16 pots
  *   IPOT_TUNE_TEST_WITHHOLD_RANK  for tests of the give-up path only: CTA `value` (0-7) of every cluster
  *                                 (IPOT_SCORER_TENSOR_SWEEPS) or of the grid (IPOT_SCORER_TENSOR), or job `value` of
  *                                 IPOT_SCORER_TENSOR_ITEMS, never reports its statistics, so every wait for them runs into
- *                                 the limit; -1 = off (default)
+ *                                 the limit; in ipot_chunk_attention half `value` (0, 1) of a thread block never reports its
+ *                                 weights; -1 = off (default)
  *   IPOT_TUNE_TEST_WITHHOLD_CHUNK for tests of the give-up path only: chunk `value` (0-7) of every tensor never reports to
  *                                 the compaction's other chunks that it has been read; -1 = off (default)
  * The compaction's waits have a limit of their own, 200 ms, which cannot be set: after one that ran out (IPOT_E_TIMEOUT, too)
@@ -390,9 +392,12 @@ int ipot_rope_rows(ipot_t *pot, const ipot_rope_t *rope, int layers, int n_token
  *   tokens : device int32 [batch], or NULL: how many tokens stream b has (below 0: none, above n_tokens: n_tokens).  The rows of
  *            out and lse behind them are left as they were, and what lies behind them in q, k and v does not count, whatever it is.
  * q_strides etc. as for ipot_rope_rows; NULL = dense in the order given.
- * Logits, softmax and sums are fp32, and in f32 pots everything is.  In bf16 pots the probabilities enter the product with
- * v as bf16 numbers relative to their row's largest (2^-8 each at most, less than the rounding of the result).
- * Asynchronous on the pot's stream; the pot is not changed.
+ * Logits, softmax and sums are fp32, and in f32 pots everything is.  In bf16 pots the weights enter the product with
+ * v as bf16 numbers (each is off by 2^-8 of itself at most, as the result is by its own rounding).  What is attended to must be finite.
+ * bf16 pots run on tensor cores: tcgen05, or for at most 8 query rows of a KV head (n_tokens * Hq / Hkv) on warp-level ones; fp32 FMAs do the rest (f32
+ * pots; Hq / Hkv > 128; inputs that repeat rows by a stride of 0).
+ * Asynchronous on the pot's stream; the pot is not changed.  A wait inside the tcgen05 kernel that runs out (see
+ * IPOT_TUNE_WAIT_LIMIT_NS) leaves out undefined and raises IPOT_E_TIMEOUT.
  * Errors: INVALID (NULL, misaligned, sizes, strides; layers outside the pot; n_tokens * (Hq / Hkv) or len + n_tokens beyond 2^30), CUDA.
  */
 int ipot_chunk_attention(ipot_t *pot, int layer, int n_layers, int n_tokens, const int32_t *tokens, const void *q,

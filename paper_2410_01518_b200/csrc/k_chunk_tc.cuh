@@ -7,7 +7,7 @@
 //   softmax     a thread owns half of a row (one warp per scheduler and stream would be a chain of latencies: 1900 cycles a tile, two 1000): p = 2^(s c - m),
 //               l += p in fp32, and p as bf16 over S in tensor memory.  The reference m is the maximum of the
 //               row's first tile; after that no maximum is taken.  fp32 and bf16 have the same exponents, so p is as exact far above 1 as below,
-//               and only a tile whose sum passes 2^60 moves the reference (the row's sums and output are then scaled down: rare).  All exponentials are the
+//               and only a tile whose sum passes 2^24 moves the reference (the row's sums and output are then scaled down: rare).  All exponentials are the
 //               special-function unit's: a quarter of them as a polynomial on the FMA pipe took 1016 us for 4 streams x 2048 tokens over 6144 rows instead of 950
 //               (in long runs the power limit holds the clock at 1.6 GHz, and what is issued costs power).
 //   O += P V    P from tensor memory, V as it lies (channels contiguous: the N-major operand layout), 128 x D fp32 in tensor memory
@@ -32,7 +32,7 @@
 namespace ipotk {
 
 constexpr int kCtRows = 128;
-constexpr float kChunkMost = 1.1529215e18f;   // 2^60: a tile's sum of a row up to here leaves the reference where it is
+constexpr float kChunkMost = 16777216.f;   // 2^24: a tile's sum of a row up to here leaves the reference where it is (and 2^100 of fp32's range to the values)
 
 template <int D, bool kSplit> struct ChunkTc {
     static constexpr int kStreams = D > 128 ? 1 : 2;
@@ -92,7 +92,7 @@ __device__ __forceinline__ bool chunk_wait(uint32_t bar, uint32_t parity, volati
     unsigned long long t0 = 0;
     for (uint32_t i = 0;; ++i) {
         if (mbar_try_wait(bar, parity)) return true;
-        if ((i & 1023u) == 1023u) {
+        if ((i & 31u) == 31u) {
             if (heed_flag && *flag) return false;
             const unsigned long long now = global_timer_ns();
             if (!t0) t0 = now;

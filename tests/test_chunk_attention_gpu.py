@@ -294,6 +294,57 @@ def test_rotary_flow_equals_attention_over_rotated_rows(interleaved):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 5, 140])
+def test_inputs_that_repeat_by_a_stride_of_zero(n, dtype):
+    """One chunk's keys and values for every stream, one query for every head (an expanded tensor, not a copy)."""
+    c = Case(dtype, 1, 3, 8, 2, 64, 150, n)
+    try:
+        c.k, c.v, c.q = c.k[:, :1].expand(1, 3, 2, n, 64), c.v[:, :1].expand(1, 3, 2, n, 64), c.q[:, :, :1].expand(1, 3, 8, n, 64)
+        assert c.k.stride(1) == 0 and c.q.stride(2) == 0
+        c.run().verify()
+    finally:
+        c.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [2, 150, 2000])
+def test_large_values_do_not_overflow_on_the_way(n):
+    """Values near the end of bf16's range, logits far above those of the row's first keys: weights and outputs are finite all the same."""
+    c = Case("bf16", 1, 2, 8, 4, 128, 1500, n)
+    try:
+        c.V.mul_(2.0 ** 80)
+        c.v.mul_(2.0 ** 80)
+        c.K[:, :, :, 700] *= 9
+        ipot.ipot_reset(c.h)
+        ipot.ipot_append_chunk(c.h, c.K, c.V, 1500)
+        c.run().verify(heads=[0, 5])
+    finally:
+        c.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", [(1, 1, 4, 1, 128, 1000, 60), (1, 1, 2, 2, 64, 300, 300), (2, 4, 32, 8, 128, 500, 400), (1, 1, 4, 1, 256, 600, 100)])
+@pytest.mark.parametrize("stream", [0, 1])
+def test_a_wait_that_runs_out_ends_the_call_and_the_next_is_right(shape, stream):
+    c = Case("bf16", *shape)
+    try:
+        ipot.ipot_set_tuning(c.h, ipot.IPOT_TUNE_WAIT_LIMIT_NS, 2_000_000)
+        ipot.ipot_set_tuning(c.h, ipot.IPOT_TUNE_TEST_WITHHOLD_RANK, stream)
+        ipot.ipot_chunk_attention(c.h, 0, shape[0], shape[6], c.q, c.k, c.v, c.out, c.lse)
+        one_stream = shape[4] > 128 and stream == 1   # (wide heads have one)
+        assert ipot.ipot_sync_status(c.h) == (0 if one_stream else ipot.IPOT_E_TIMEOUT)
+        ipot.ipot_set_tuning(c.h, ipot.IPOT_TUNE_TEST_WITHHOLD_RANK, -1)
+        ipot.ipot_set_tuning(c.h, ipot.IPOT_TUNE_WAIT_LIMIT_NS, 200_000_000)
+        c.out.fill_(5)
+        ipot.ipot_chunk_attention(c.h, 0, shape[0], shape[6], c.q, c.k, c.v, c.out, c.lse)
+        torch.cuda.synchronize()
+        c.verify(heads=[0, shape[2] - 1])
+    finally:
+        c.close()
+
+
+@pytest.mark.gpu
 def test_refusals_leave_everything_alone():
     c = Case("bf16", 2, 1, 4, 2, 64, 10, 8)
     try:
