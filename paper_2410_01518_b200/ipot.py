@@ -12,6 +12,7 @@ it is built when ``nvcc`` is available; there is no fallback implementation.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 from . import build as _build
@@ -128,11 +129,10 @@ def lib() -> C.CDLL:
 def _ptr(x):
     if x is None:
         return None
-    if hasattr(x, "data_ptr"):
-        return x.data_ptr()
-    if hasattr(x, "ctypes"):
-        return x.ctypes.data
-    return int(x)
+    try:
+        return x.data_ptr()   # (no test first: a generated token's calls are a few microseconds long)
+    except AttributeError:
+        return x.ctypes.data if hasattr(x, "ctypes") else int(x)
 
 
 def _check(rc: int, what: str) -> int:
@@ -242,9 +242,14 @@ def ipot_view_rope(h) -> int:
     return p.value
 
 
+@functools.lru_cache(maxsize=1024)
+def _strides_of(s):
+    return C.byref(ipot_strides_t(*s))
+
+
 def _strides(s):
     """(layer, stream, head, token) in elements, or None: dense."""
-    return None if s is None else C.byref(ipot_strides_t(*s))
+    return None if s is None else _strides_of(tuple(s))
 
 
 def ipot_rope_tables(cos_table, sin_table, first, n, rotary_dim, dtype, base=10000.0, scaling=IPOT_ROPE_PLAIN, factor=1.0,
