@@ -32,6 +32,7 @@
 namespace ipotk {
 
 constexpr int kCtRows = 128;
+constexpr unsigned long long kChunkLandNs = 200ull * 1000 * 1000;
 constexpr float kChunkMost = 16777216.f;   // 2^24: a tile's sum of a row up to here leaves the reference where it is (and 2^100 of fp32's range to the values)
 
 template <int D, bool kSplit> struct ChunkTc {
@@ -48,10 +49,12 @@ template <int D, bool kSplit> struct ChunkTc {
     static constexpr uint32_t kOutCol = 256;                                 // tensor memory: S of stream i at 128 i, O at 256 + D i
     static constexpr int kThreads = 64 + 256 * kStreams;
     static constexpr int kCols = kKeys / 2;                                  // of a softmax thread
-    static_assert(kCtRows * kPitch * 4 <= kStages * kStageBytes, "partial results take the stages' place");
+    static constexpr bool kPush = D <= 128;                                  // room for what the cluster's other blocks send
+    static constexpr uint32_t kPartBytes = kCtRows * kPitch * 4;
+    static_assert(kPartBytes <= kStages * kStageBytes && (!kPush || 2 * kPartBytes + 8 * kPitch * 4 <= kStages * kStageBytes), "partial results take the stages' place");
     static_assert(kSmemBytes <= 232448, "shared memory of a block");
 };
-enum { kCbQ = 0, kCbFull = 1, kCbEmpty = 9, kCbS = 17, kCbP = 19, kCbO = 21, kCbDrain = 23, kCbCount = 24 };
+enum { kCbQ = 0, kCbFull = 1, kCbEmpty = 9, kCbS = 17, kCbP = 19, kCbO = 21, kCbDrain = 23, kCbMerge = 24, kCbCount = 25 };
 
 // D[M x N] += A B with A in tensor memory (a row per lane, two bf16 per column).
 __device__ __forceinline__ void tc_mma_bf16_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate)
@@ -86,7 +89,8 @@ __device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&v)[32
           "r"(taddr) : "memory");
 }
 
-// A wait of at most wait_ns from its start.  flag: the block's give-up flag; with heed_flag off it is a role's wait for what it has itself put in flight.
+// A wait of at most wait_ns from its start.  flag: the block's give-up flag; with heed_flag off it is a wait for what is in flight and will land, which the block must not end before (its
+// limit is never less than 200 ms).
 __device__ __forceinline__ bool chunk_wait(uint32_t bar, uint32_t parity, volatile int *flag, const ChunkTcParams &p, bool heed_flag = true)
 {
     unsigned long long t0 = 0;
@@ -96,7 +100,7 @@ __device__ __forceinline__ bool chunk_wait(uint32_t bar, uint32_t parity, volati
             if (heed_flag && *flag) return false;
             const unsigned long long now = global_timer_ns();
             if (!t0) t0 = now;
-            if (now - t0 > p.wait_ns) {
+            if (now - t0 > (heed_flag ? p.wait_ns : max(p.wait_ns, kChunkLandNs))) {
                 *flag = 1;
                 set_status(p.status, kStatusTimeout);
                 return false;
@@ -223,6 +227,10 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
     const int units = p.c.layers * p.c.streams * p.c.Hkv, item = blockIdx.x / ranks, unit = item % units;
     const int tile0 = (p.items_per_unit - 1 - item / units) * L::kQTiles;   // of kCtRows rows: p.tile_tokens tokens
     const int hkv = unit % p.c.Hkv, b = unit / p.c.Hkv % p.c.streams, l = unit / p.c.Hkv / p.c.streams;
+    if (warp == 2 && lane < 5) {   // (the maps are parameters: they can be fetched before anything else is there)
+        const CUtensorMap *maps[5] = {&mapQ, &mapK, &mapV, &mapKnew, &mapVnew};
+        asm volatile("prefetch.tensormap [%0];" ::"l"(maps[lane]) : "memory");
+    }
     if (threadIdx.x == 0) {
         *flag = 0;
         for (int i = 0; i < kCbCount; ++i) mbar_init(bar(i), i >= kCbP && i < kCbO ? 8 : 1);   // (P: a stream's eight warps)
@@ -499,41 +507,55 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
             }
         }
         if (ranks > 1) {
-            cluster_sync();
-            // a thread has 8 channels of a row; four blocks' values of them on their way at once
-            const int vecs = p.c.d / 8, rows = max(tokens[0], 0) * G;
-            for (int e = rank * L::kThreads + threadIdx.x; e < rows * vecs; e += ranks * L::kThreads) {
-                const int row = e / vecs, v = e - row * vecs;
+            // Every block of the cluster owns some rows.  Their results come to it as one copy of shared memory from each of the others (L::kPush), or, where there is no room for
+            // that, it reads them there (64 tokens over 8000 rows, clusters of 7: reading everything, statistics per vector, 33.6 us, now 26.7).
+            const int vecs = p.c.d / 8, rows = max(tokens[0], 0) * G, per = (rows + (int)ranks - 1) / (int)ranks, mine_from = min(rows, (int)rank * per), mine_rows = min(rows, mine_from + per) - mine_from;
+            float *got = part + L::kPartBytes / 4;
+            float2 *stats = reinterpret_cast<float2 *>(ct_raw + L::kOffQ);   // [blocks][own rows]
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            cluster_sync();   // all results are there, and nobody's stages are in use any more
+            if (L::kPush && threadIdx.x == 0 && tiles > 0) {
+                for (uint32_t o = 0; o < ranks; ++o) {
+                    const int from = min(rows, (int)o * per), n_rows = min(rows, from + per) - from;
+                    if (n_rows <= 0) continue;
+                    asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(cluster_addr(got + (size_t)rank * per * L::kPitch, o)),
+                                 "r"(smem_u32(part + (size_t)from * L::kPitch)), "r"((uint32_t)n_rows * L::kPitch * 4u), "r"(cluster_addr(ct_raw + L::kOffBar + 8 * kCbMerge, o)) : "memory");
+                }
+            }
+            for (int e = threadIdx.x; e < mine_rows * (int)ranks; e += L::kThreads) {
+                const int k = e / mine_rows;
+                stats[e] = cluster_ld2(cluster_addr(&stat[mine_from + e - k * mine_rows], k));
+            }
+            if (L::kPush && mine_rows > 0) {
+                // (blocks that have had no key tile send nothing)
+                if (threadIdx.x == 0) mbar_expect_tx(bar(kCbMerge), (uint32_t)min((int)ranks, all_tiles) * (uint32_t)mine_rows * L::kPitch * 4u);
+                chunk_wait(bar(kCbMerge), 0, flag, p, false);
+            }
+            __syncthreads();
+            // a thread has 8 channels of a row
+            for (int e = threadIdx.x; e < mine_rows * vecs; e += L::kThreads) {
+                const int r = e / vecs, v = e - r * vecs, row = mine_from + r;
                 float ref = -INFINITY, den = 0.f, o[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) o[k] = 0.f;
-                for (uint32_t r0 = 0; r0 < ranks; r0 += 4) {   // (1, 2, 4 or 8 blocks)
-                    float2 st[4];
-                    float4 x[4], y[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const uint32_t r = min(r0 + k, ranks - 1), src = cluster_addr(part + (size_t)row * L::kPitch + 8 * v, r);
-                        st[k] = cluster_ld2(cluster_addr(&stat[row], r));
-                        x[k] = cluster_ld4(src);
-                        y[k] = cluster_ld4(src + 16);
-                        if (r0 + k >= ranks) st[k] = make_float2(-INFINITY, 0.f);
+                for (uint32_t k = 0; k < ranks; ++k) ref = fmaxf(ref, stats[k * mine_rows + r].x);
+                for (uint32_t k = 0; k < ranks; ++k) {
+                    const float2 st = stats[k * mine_rows + r];
+                    if (st.x == -INFINITY) continue;   // it has seen no key of this row: what it holds is not a number
+                    float4 x, y;
+                    if (L::kPush) {
+                        const float4 *src = reinterpret_cast<const float4 *>(got + (size_t)(k * per + r) * L::kPitch + 8 * v);
+                        x = src[0];
+                        y = src[1];
+                    } else {
+                        const uint32_t src = cluster_addr(part + (size_t)row * L::kPitch + 8 * v, k);
+                        x = cluster_ld4(src);
+                        y = cluster_ld4(src + 16);
                     }
-                    float top = ref;
+                    const float f = chunk_ex2(st.x - ref), z[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+                    den = fmaf(st.y, f, den);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) top = fmaxf(top, st[k].x);
-                    const float fr = ref == -INFINITY ? 0.f : chunk_ex2(ref - top);
-                    ref = top;
-                    den *= fr;
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) o[k] *= fr;
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        if (st[k].x == -INFINITY) continue;   // it has seen no key of this row: what it holds is not a number
-                        const float f = chunk_ex2(st[k].x - ref), z[8] = {x[k].x, x[k].y, x[k].z, x[k].w, y[k].x, y[k].y, y[k].z, y[k].w};
-                        den = fmaf(st[k].y, f, den);
-#pragma unroll
-                        for (int c = 0; c < 8; ++c) o[c] = fmaf(z[c], f, o[c]);
-                    }
+                    for (int c = 0; c < 8; ++c) o[c] = fmaf(z[c], f, o[c]);
                 }
                 const float inv = 1.f / den;
                 uint32_t w[4];
@@ -547,7 +569,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                 *reinterpret_cast<uint4 *>(out + 8 * v) = make_uint4(w[0], w[1], w[2], w[3]);
                 if (v == 0 && p.c.lse) p.c.lse[(((size_t)l * p.c.streams + b) * p.c.Hkv * G + hkv * G + g) * p.c.n + t] = 0.6931471805599453f * (ref + log2f(den));
             }
-            cluster_sync();   // no block ends while others read its results
+            cluster_sync();   // no block ends while others read or send
         }
     }
     tc_fence_before();

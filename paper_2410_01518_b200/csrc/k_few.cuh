@@ -91,7 +91,7 @@ __device__ __forceinline__ unsigned long long order_key64(double s)
 // The ascending list of the `need` largest of `others` keys (ties: the lower block); a thread has up to KPT neighbouring blocks.  The keys are taken apart at
 // the highest bit in which they differ: 32 bits from there decide nearly always, those below them where that leaves a tie.  Two bits a step: three counts
 // in one sum over the warp, one barrier a step, and the search ends as soon as a count is right.  (One warp with 8 keys a lane and no barrier: 600 cycles
-// a step, this 130.)
+// a step, this 300.)
 template <int KPT>
 __device__ __forceinline__ void select_in_block(FewShared &sh, const double *score, int others, int need)
 {
@@ -211,7 +211,7 @@ __device__ __forceinline__ int select_blocks(FewShared &sh, uint8_t *free_bytes,
         return want;
     }
     // this block's share of the others: their bounds come into shared memory, as many at once as find room.  (Straight into registers, four blocks a warp and four more on their
-    // way, the loads were a chain of latencies: 256 units x 127 blocks x 128 channels 41 us for the call, 33 so.)
+    // way, the loads were a chain of latencies: 256 units x 127 blocks x 128 channels 41.0 us for the call, 38.4 so.)
     const T *lo = (const T *)p.lo + (size_t)u.unit * p.unit_blocks * p.d, *hi = (const T *)p.hi + (size_t)u.unit * p.unit_blocks * p.d;
     const int mine0 = (int)((long long)others * u.rank / u.ranks), mine = (int)((long long)others * (u.rank + 1) / u.ranks) - mine0, room = room_bytes / (2 * p.d * (int)sizeof(T));
     auto fetch = [&](int from) {
