@@ -394,7 +394,7 @@ int ipot_rope_rows(ipot_t *pot, const ipot_rope_t *rope, int layers, int n_token
  * q_strides etc. as for ipot_rope_rows; NULL = dense in the order given.
  * Logits, softmax and sums are fp32, and in f32 pots everything is.  In bf16 pots the weights enter the product with
  * v as bf16 numbers (each is off by 2^-8 of itself at most, as the result is by its own rounding).  What is attended to must be finite.
- * bf16 pots run on tensor cores: tcgen05, or for at most 8 query rows of a KV head (n_tokens * Hq / Hkv) on warp-level ones; fp32 FMAs do the rest (f32
+ * bf16 pots run on tensor cores: tcgen05, or for a handful of query rows of a KV head (n_tokens * Hq / Hkv) on warp-level ones; fp32 FMAs do the rest (f32
  * pots; Hq / Hkv > 128; inputs that repeat rows by a stride of 0).
  * Asynchronous on the pot's stream; the pot is not changed.  A wait inside the tcgen05 kernel that runs out (see
  * IPOT_TUNE_WAIT_LIMIT_NS) leaves out undefined and raises IPOT_E_TIMEOUT.

@@ -1,4 +1,4 @@
-// Attention of at most 8 query rows of a KV head over many keys: generation.  Two calls come here:
+// Attention of at most 8 query rows of a KV head (or twice as many, in two groups) over many keys: generation.  Two calls come here:
 //   a chunk of few tokens (kSparse = false): rows t * G + g over the pot's rows and the chunk's rows 0 .. t;
 //   one token over selected blocks of the pot (kSparse = true; the query heads of a KV head in groups of 8).
 // Either is a stream of keys and values through few rows, split over a thread-block cluster per unit: bound by HBM, or where there
@@ -390,7 +390,7 @@ template <bool kSparse> struct FewTiles {
     __device__ __forceinline__ FewTiles(const FewParams &p, const FewUnit &u, int selected)
     {
         pot = kSparse ? selected * (p.block_rows / 16) : (p.len + 15) / 16;
-        all = kSparse ? pot : pot + 1;   // (at most 8 tokens)
+        all = kSparse ? pot : pot + 1;   // (at most 16 tokens)
     }
     // first row and number of rows (0: none are there); fresh: they are the chunk's
     __device__ __forceinline__ void locate(const FewParams &p, const FewUnit &u, const uint16_t *list, int tile, int &row, int &count, bool &fresh) const
@@ -694,7 +694,7 @@ few_fma_kernel(const __grid_constant__ FewParams p, int lpk)
                     va = V + (size_t)i * vecs;
                 } else {
                     const int t = i - p.len;
-                    seen_by[j] = t * p.G;   // (row0 is 0)
+                    seen_by[j] = min(t * p.G - u.row0, R);   // (below 0: all)
                     ka = Kn + t * (p.ks.token / VE);
                     va = Vn + t * (p.vs.token / VE);
                 }

@@ -27,11 +27,16 @@ cudaError_t launch_rope_rows(const RopeRowsParams &p, bool f32, bool table_f32, 
     return interleaved ? launch_rope_rows_t<bf16, bf16, true>(p, stream) : launch_rope_rows_t<bf16, bf16, false>(p, stream);
 }
 
-// Few rows have a kernel of their own; else tensor cores for bf16, unless a group's heads do not fit into one tile of query rows or the strides are none that a tensor map
+// Few rows have a kernel of their own: up to 8 of a KV head, or two groups of 8 that each go over the keys, as long as the second finds them in L2 (bf16, 8 heads a
+// KV head of 128 channels, us, this / tcgen05: 16 rows, 8 units x 4095 keys 11.6 / 15.8, 64 units 33.5 / 35.1, 256 units 152 / 117; 8 units x 16000 25.6 / 27.0, 64 units 103 / 91).
+// Else tensor cores for bf16, unless a group's heads do not fit into one tile of query rows or the strides are none that a tensor map
 // takes (an input whose rows repeat by a stride of 0).
 cudaError_t launch_chunk_attention(const ChunkParams &p, bool f32, const ChunkTcHost &host, cudaStream_t stream)
 {
-    if (p.n * p.G <= kFewRows) {
+    constexpr double kStaysInL2 = 134e6;
+    const int rows = p.n * p.G;   // (at most 2^30)
+    const double key_bytes = 2.0 * p.layers * p.streams * p.Hkv * ((double)p.len + p.n) * p.d * (f32 ? 4 : 2);
+    if (rows <= kFewRows || (rows <= 2 * kFewRows && key_bytes <= kStaysInL2)) {
         FewParams f = {};
         f.q = p.q; f.qs = p.qs; f.K = p.potK; f.V = p.potV;
         f.unit0 = p.unit0; f.unit_rows = p.unit_rows; f.len = p.len;

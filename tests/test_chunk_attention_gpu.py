@@ -118,7 +118,7 @@ SHAPES = [
     (1, 1, 8, 2, 128, 0, 300), (1, 2, 4, 2, 128, 128, 128), (2, 1, 4, 2, 128, 127, 129), (1, 1, 2, 2, 128, 1000, 255), (1, 1, 6, 2, 128, 65, 77),
     (1, 1, 5, 1, 64, 333, 100), (1, 3, 12, 4, 96, 199, 33), (1, 1, 7, 1, 32, 64, 64), (1, 1, 3, 3, 40, 513, 130), (1, 1, 8, 1, 72, 100, 50),
     (1, 1, 4, 2, 256, 400, 129), (1, 1, 2, 1, 192, 30, 65), (1, 1, 16, 1, 136, 257, 19), (1, 1, 16, 1, 128, 129, 40), (1, 1, 48, 1, 64, 200, 9),
-    (1, 1, 136, 1, 64, 70, 3), (1, 1, 1, 1, 256, 1500, 1), (1, 1, 8, 8, 64, 2047, 65), (3, 2, 2, 1, 248, 5, 70),
+    (1, 1, 136, 1, 64, 70, 3), (1, 2, 8, 2, 128, 600, 4), (1, 1, 16, 1, 64, 100, 1), (2, 1, 5, 1, 96, 333, 3), (1, 1, 1, 1, 40, 50, 16), (1, 1, 12, 1, 256, 70, 1), (1, 1, 1, 1, 256, 1500, 1), (1, 1, 8, 8, 64, 2047, 65), (3, 2, 2, 1, 248, 5, 70),
 ]
 
 
