@@ -5,9 +5,9 @@
 // first the pot's, then the chunk's.  Per tile and stream
 //   S = Q K^T   128 x KT fp32 in tensor memory (both operands in shared memory, K-major, 128-byte swizzle)
 //   softmax     a thread owns half of a row (one warp per scheduler and stream would be a chain of latencies: 1900 cycles a tile, two 1000): p = 2^(s c - m),
-//               l += p in fp32, and p as bf16 over S in tensor memory.  The reference m is the maximum of the
-//               row's first tile; after that no maximum is taken.  fp32 and bf16 have the same exponents, so p is as exact far above 1 as below,
-//               and only a tile whose sum passes 2^24 moves the reference (the row's sums and output are then scaled down: rare).  All exponentials are the
+//               l += p in fp32, and p as bf16 over S in tensor memory.  No maximum is taken: fp32 and bf16 have the same exponents, so p is as exact far above 1
+//               as below.  The reference m is 0 unless the sum of the row's first tile is far from 1, and only a later tile whose sum passes 2^24 moves it (the row's sums and output
+//               are then scaled down).  Tiles with columns that some row does not see, and those two kinds, take a general form that does take the maximum.  All exponentials are the
 //               special-function unit's: a quarter of them as a polynomial on the FMA pipe took 1016 us for 4 streams x 2048 tokens over 6144 rows instead of 950
 //               (in long runs the power limit holds the clock at 1.6 GHz, and what is issued costs power).
 //   O += P V    P from tensor memory, V as it lies (channels contiguous: the N-major operand layout), 128 x D fp32 in tensor memory
@@ -34,6 +34,7 @@ namespace ipotk {
 constexpr int kCtRows = 128;
 constexpr unsigned long long kChunkLandNs = 200ull * 1000 * 1000;
 constexpr float kChunkMost = 16777216.f;   // 2^24: a tile's sum of a row up to here leaves the reference where it is (and 2^100 of fp32's range to the values)
+constexpr float kChunkLeast = 5.9604645e-8f;  // 2^-24: a first tile's sum from here on lets the reference be 0
 
 template <int D, bool kSplit> struct ChunkTc {
     static constexpr int kStreams = D > 128 ? 1 : 2;
@@ -121,7 +122,8 @@ __device__ __forceinline__ bool chunk_pair_any(int id, bool x)
     return r != 0;
 }
 
-// A tile of a warp's rows in general: its first (the row's maximum becomes the reference), one with columns that some row does not see, and one that left the range.
+// A tile of a warp's rows in general: one with columns that some row does not see, a first one whose sum is far from 1, and one that left the range: the row's maximum
+// becomes the reference if it is above it.
 // W columns from ts on, of which this row sees `cols`; the other warp of the pair has the other half and takes part.  seen: the row's two maxima.  scale: whether O
 // holds something already (W2 columns of it from `to` on are this warp's).  Leaves p over the first half of its columns; (reference, sum).
 template <int W, int W2>
@@ -387,12 +389,13 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
             __syncwarp();
             tc_fence_after();
             if (works) {
-                bool general = j == 0 || masked;
+                bool general = masked;
                 if (!general) {
                     uint32_t h[W / 32][16];
-                    const float s = chunk_tile<W>(ts, c, m, h);
-                    general = chunk_pair_any(pair, valid && !(s < kChunkMost));   // (the logits are still there)
+                    const float ref = j ? m : 0.f, s = chunk_tile<W>(ts, c, ref, h);
+                    general = chunk_pair_any(pair, valid && !(s < kChunkMost && (j || s > kChunkLeast)));   // (the logits are still there)
                     if (!general) {
+                        m = ref;
                         sum += s;
 #pragma unroll
                         for (int a = 0; a < W / 32; ++a) tmem_st16(ts + 16 * a, h[a]);
