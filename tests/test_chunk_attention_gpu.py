@@ -260,6 +260,7 @@ def test_rotary_flow_equals_attention_over_rotated_rows(interleaved):
     Kr, Vr = torch.empty((L, B, Hkv, 0, d), dtype=bf, device="cuda"), torch.empty((L, B, Hkv, 0, d), dtype=bf, device="cuda")
     try:
         ipot.ipot_enable_rope(h, cos, sin, pairing)
+        ipot.ipot_enable_blocks(h, 16)
 
         def step(m):
             nonlocal Kr, Vr
@@ -289,8 +290,56 @@ def test_rotary_flow_equals_attention_over_rotated_rows(interleaved):
         Vr = ipot.device_array(ipot.ipot_view(h)[1], (L, B, Hkv, size, d), "bf16")[:, :, :, :100].clone()
         step(1)
         step(60)
+        # one generated token: over the pot, over all of its blocks, over some of them.  Outputs are fp32: the head's bound for f32, and
+        # weights in two bf16 terms (over the pot, 2^-16 A) or three (over blocks, 2^-22 A).
+        q = torch.randn((L, B, Hq, d), generator=g, device="cuda").to(bf)
+        blocks = torch.zeros((L, B, Hkv, 3), dtype=torch.int32, device="cuda")
+        for kind in ("pot", "all", "some"):
+            out, lse = torch.zeros((L, B, Hq, d), device="cuda"), torch.zeros((L, B, Hq), device="cuda")
+            if kind == "pot":
+                ipot.ipot_decode_attention(h, q, out, lse)
+            else:
+                ipot.ipot_decode_attention_blocks(h, 0, L, q, *((11, out, lse) if kind == "all" else (3, out, lse, blocks)))   # 161 rows
+            assert ipot.ipot_sync_status(h) == 0
+            for b in range(B):
+                for hh in range(Hq):
+                    kv = hh // (Hq // Hkv)
+                    at = torch.arange(161) if kind != "some" else torch.cat([torch.arange(int(i) * 16, min(161, int(i) * 16 + 16)) for i in blocks[0, b, kv]])
+                    K, V, qd = Kr[0, b, kv][at.cuda()].double(), Vr[0, b, kv][at.cuda()].double(), q[0, b, hh].double()
+                    x = K @ qd / math.sqrt(d)
+                    w, N = torch.softmax(x, 0), len(at)
+                    dx, A = (d + 4) * 2.0 ** -23 * float((K.abs() @ qd.abs()).max()) / math.sqrt(d), w @ V.abs()
+                    tol = A * (4 * dx + 2.0 ** -20 + 2 * N * 2.0 ** -24 + (2.0 ** -16 if kind == "pot" else 2.0 ** -22)) + 2.0 ** -24 * (w @ V).abs()
+                    assert bool(((w @ V - out[0, b, hh]).abs() <= tol).all())
+                    want = float(torch.logsumexp(x, 0))
+                    assert abs(want - float(lse[0, b, hh])) <= 2 * dx + 2.0 ** -20 + N * 2.0 ** -24 + 2.0 ** -22 * abs(want)
+        assert bool((blocks[..., 2] == 10).all())
     finally:
         ipot.ipot_destroy(h)
+
+
+@pytest.mark.gpu
+def test_two_pots_on_two_streams_at_once():
+    """Calls that overlap on the GPU give what they give alone: nothing is shared."""
+    cases = [Case("bf16", 1, 1, 8, 2, 128, 3000, 1, seed=1), Case("bf16", 1, 1, 8, 2, 128, 3000, 60, seed=2), Case("bf16", 1, 2, 8, 2, 64, 900, 700, seed=3), Case("f32", 1, 1, 8, 2, 64, 500, 90, seed=4)]
+    try:
+        want = [c.run().out.clone() for c in cases]
+        streams = [torch.cuda.Stream() for _ in cases]
+        torch.cuda.synchronize()
+        for c, s in zip(cases, streams):
+            ipot.ipot_set_stream(c.h, s.cuda_stream)
+            c.out.fill_(0)
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for c in cases:
+                ipot.ipot_chunk_attention(c.h, 0, 1, c.n, c.q, c.k, c.v, c.out, c.lse)
+        torch.cuda.synchronize()
+        for c, w in zip(cases, want):
+            assert ipot.ipot_sync_status(c.h) == 0 and torch.equal(c.out, w)
+    finally:
+        torch.cuda.synchronize()
+        for c in cases:
+            c.close()
 
 
 @pytest.mark.gpu
