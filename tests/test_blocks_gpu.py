@@ -116,6 +116,29 @@ def test_shapes(shape, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("early", [False, True])   # bounds taken along by the appends, or from the rows that are there
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_layer_behind_two_to_the_31_elements(dtype, early):
+    """520 units of 32768 slots of 128 channels: the last layer's rows start behind element 2^31 of the pot."""
+    cfg = config(dtype, 65, 1, 16, 8, 128, 32768)
+    g = torch.Generator(device="cuda").manual_seed(12)
+    K, V = (torch.randn((65, 1, 8, 200, 128), generator=g, device="cuda").to(DT[dtype]) for _ in range(2))
+    q = torch.randn((1, 1, 16, 128), generator=g, device="cuda").to(DT[dtype])
+    h = make_pot(cfg)
+    try:
+        if early:
+            ipot.ipot_enable_blocks(h, 16)
+        for part in (slice(0, 90), slice(90, 200)):
+            ipot.ipot_append_chunk(h, K[:, :, :, part].contiguous(), V[:, :, :, part].contiguous(), part.stop - part.start)
+        if not early:
+            ipot.ipot_enable_blocks(h, 16)
+        out, lse, blocks = attend(h, cfg, q, 5, layer=64)
+        verify(cfg, q, K[64:], V[64:], 16, 5, out, lse, blocks)
+    finally:
+        ipot.ipot_destroy(h)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype,n,R,n_blocks", [("bf16", 32768, 16, 300), ("bf16", 16384, 64, 32), ("f32", 20000, 16, 64), ("bf16", 32767, 16, 2000), ("bf16", 30000, 128, 17)])
 def test_long_pots(dtype, n, R, n_blocks):
     cfg = config(dtype, 1, 1, 16, 4, 128, n)

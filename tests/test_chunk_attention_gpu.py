@@ -201,6 +201,19 @@ def test_long(dtype, shape):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("n", [1, 40])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_layer_behind_two_to_the_31_elements(dtype, n):
+    """520 units of 32768 slots of 128 channels: the last layer's rows start behind element 2^31 of the pot."""
+    c = Case(dtype, 65, 1, 16, 8, 128, 200, n, pot_size=32768)
+    try:
+        c.run(layer=64, layers=1).verify(layers=[64], heads=[0, 15])
+        assert bool((c.out[:64] == 5).all() and (c.lse[:64] == 5).all())
+    finally:
+        c.close()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_the_same_call_gives_the_same_bits(dtype):
     for shape in ((1, 1, 8, 2, 128, 4000, 1), (1, 1, 8, 2, 128, 1500, 200)):
@@ -319,7 +332,7 @@ def test_rotary_flow_equals_attention_over_rotated_rows(interleaved):
 
 
 @pytest.mark.gpu
-def test_two_pots_on_two_streams_at_once():
+def test_pots_on_streams_of_their_own_at_once():
     """Calls that overlap on the GPU give what they give alone: nothing is shared."""
     cases = [Case("bf16", 1, 1, 8, 2, 128, 3000, 1, seed=1), Case("bf16", 1, 1, 8, 2, 128, 3000, 60, seed=2), Case("bf16", 1, 2, 8, 2, 64, 900, 700, seed=3), Case("f32", 1, 1, 8, 2, 64, 500, 90, seed=4)]
     try:
