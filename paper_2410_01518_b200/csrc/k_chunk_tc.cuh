@@ -7,7 +7,7 @@
 //   softmax     a thread owns half of a row (one warp per scheduler and stream would be a chain of latencies: 1900 cycles a tile, two 1000): p = 2^(s c - m),
 //               l += p in fp32, and p as bf16 over S in tensor memory.  No maximum is taken: fp32 and bf16 have the same exponents, so p is as exact far above 1
 //               as below.  The reference m is 0 unless the sum of the row's first tile is far from 1, and only a later tile whose sum passes 2^24 moves it (the row's sums and output
-//               are then scaled down).  Tiles with columns that some row does not see, and those two kinds, take a general form that does take the maximum.  All exponentials are the
+//               are then scaled down).  Tiles with columns that some row does not see, those two kinds, and those of a row whose reference is beyond 2^24, take a general form that does take the maximum.  All exponentials are the
 //               special-function unit's: a quarter of them as a polynomial on the FMA pipe took 1016 us for 4 streams x 2048 tokens over 6144 rows instead of 950
 //               (in long runs the power limit holds the clock at 1.6 GHz, and what is issued costs power).
 //   O += P V    P from tensor memory, V as it lies (channels contiguous: the N-major operand layout), 128 x D fp32 in tensor memory
@@ -35,6 +35,11 @@ constexpr int kCtRows = 128;
 constexpr unsigned long long kChunkLandNs = 200ull * 1000 * 1000;
 constexpr float kChunkMost = 16777216.f;   // 2^24: a tile's sum of a row up to here leaves the reference where it is (and 2^100 of fp32's range to the values)
 constexpr float kChunkLeast = 5.9604645e-8f;  // 2^-24: a first tile's sum from here on lets the reference be 0
+// A reference is a rounded product, and s c, not rounded before the reference is subtracted, misses it by up to half its last place: 1 and more from 2^24 on, further out more than the
+// exponential's range.  The general form rounds the product, so that the row's maximum comes out as exactly 0; near 0 that is as good.  From here on a row takes nothing else: its reference
+// then waits in its threads' shared memory and is NaN in their registers, so that a plain tile's sum is NaN and the check that there is fails.  (4 streams x 2048 tokens over 6144 rows
+// 953.4 -> 954.4 us, 2048 tokens into an empty pot 45.0 -> 45.6; a compare per tile and a flag across them cost 4.5 %.)
+constexpr float kChunkFar = 16777216.f;       // 2^24
 
 template <int D, bool kSplit> struct ChunkTc {
     static constexpr int kStreams = D > 128 ? 1 : 2;
@@ -122,13 +127,15 @@ __device__ __forceinline__ bool chunk_pair_any(int id, bool x)
     return r != 0;
 }
 
-// A tile of a warp's rows in general: one with columns that some row does not see, a first one whose sum is far from 1, and one that left the range: the row's maximum
-// becomes the reference if it is above it.
-// W columns from ts on, of which this row sees `cols`; the other warp of the pair has the other half and takes part.  seen: the row's two maxima.  scale: whether O
-// holds something already (W2 columns of it from `to` on are this warp's).  Leaves p over the first half of its columns; (reference, sum).
+// A tile of a warp's rows in general: one with columns that some row does not see, a first one whose sum is far from 1, one that left the range, and every one of a row with a far
+// reference: the row's maximum becomes the reference if it is above it.
+// W columns from ts on, of which this row sees `cols`; the other warp of the pair has the other half and takes part.  seen: the row's two maxima and, between two tiles, a far reference, each
+// thread's in its half.  scale: whether O holds something already (W2 columns of it from `to` on are this warp's).  Leaves p over the first half of its columns; (reference or NaN, sum).
 template <int W, int W2>
 __device__ __noinline__ float2 chunk_tile_general(uint32_t ts, uint32_t to, int cols, float c, float m, float sum, bool valid, bool scale, float2 *seen, int half, int pair)
 {
+    float *mine = half ? &seen->y : &seen->x;
+    if (isnan(m)) m = *mine;
     uint32_t v[W / 32][32];
     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -143,7 +150,7 @@ __device__ __noinline__ float2 chunk_tile_general(uint32_t ts, uint32_t to, int 
         }
     }
     float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-    (half ? seen->y : seen->x) = top;
+    *mine = top;
     chunk_pair_sync(pair);
     top = fmaxf(seen->x, seen->y) * c;
     const bool moves = valid && top > m;
@@ -171,13 +178,18 @@ __device__ __noinline__ float2 chunk_tile_general(uint32_t ts, uint32_t to, int 
         uint32_t h[16];
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
-            const float x = chunk_ex2(fmaf(__uint_as_float(v[a][e]), c, -ref)), y = chunk_ex2(fmaf(__uint_as_float(v[a][e + 1]), c, -ref));   // (-inf: 0)
+            const float x = chunk_ex2(__fmul_rn(__uint_as_float(v[a][e]), c) - ref), y = chunk_ex2(__fmul_rn(__uint_as_float(v[a][e + 1]), c) - ref);   // (-inf: 0)
             s[e & 2] += x;
             s[(e & 2) + 1] += y;
             const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
             h[e >> 1] = *reinterpret_cast<const uint32_t *>(&b);
         }
         tmem_st16(ts + 16 * a, h);
+    }
+    chunk_pair_sync(pair);   // both maxima have been read (every call has the same barriers, whatever the two warps have read: after a wait that ran out they no longer go in step)
+    if (fabsf(ref) >= kChunkFar) {
+        *mine = m;
+        m = NAN;
     }
     return make_float2(m, sum + ((s[0] + s[1]) + (s[2] + s[3])));
 }
@@ -418,6 +430,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
             tc_fence_after();
         }
         if (works) {   // the two halves' sums
+            if (isnan(m)) m = half ? stat->y : stat->x;   // (a far reference)
             (half ? stat->y : stat->x) = sum;
             chunk_pair_sync(pair);
             sum = stat->x + stat->y;
