@@ -393,7 +393,8 @@ int ipot_rope_rows(ipot_t *pot, const ipot_rope_t *rope, int layers, int n_token
  *            out and lse behind them are left as they were, and what lies behind them in q, k and v does not count, whatever it is.
  * q_strides etc. as for ipot_rope_rows; NULL = dense in the order given.
  * Logits, softmax and sums are fp32, and in f32 pots everything is.  In bf16 pots the weights enter the product with
- * v as bf16 numbers (each is off by 2^-8 of itself at most, as the result is by its own rounding).  What is attended to must be finite.
+ * v as bf16 numbers (each is off by 2^-8 of itself at most, as the result is by its own rounding).  What is attended to must be finite, its
+ * logits in fp32 too, and values at most 2^127 in size (weights are scaled so that nothing overflows on the way; below 2^-65 values may lose bits).
  * bf16 pots run on tensor cores: tcgen05, or for a handful of query rows of a KV head (n_tokens * Hq / Hkv) on warp-level ones; fp32 FMAs do the rest (f32
  * pots; Hq / Hkv > 128; inputs that repeat rows by a stride of 0).
  * Asynchronous on the pot's stream; the pot is not changed.  A wait inside the tcgen05 kernel that runs out (see
@@ -430,7 +431,8 @@ int ipot_view_blocks(ipot_t *pot, void **lo, void **hi, int *n_blocks);
  *                 selected rows
  *   blocks      : device int32 [n_layers][batch][Hkv][n_blocks], or NULL: the chosen blocks in ascending order, -1 behind the last
  *                 where the pot has fewer than n_blocks blocks (all are then chosen)
- * Everything is fp32 where not said otherwise.  All inputs must be finite.  Asynchronous on the pot's stream; the pot is not changed.
+ * Everything is fp32 where not said otherwise.  All inputs must be finite, their logits in fp32 too, and values at most 2^127 in size.
+ * Asynchronous on the pot's stream; the pot is not changed.
  * Errors: INVALID (NULL, misaligned, layers outside the pot, n_blocks < 1 or > ceil(pot_size / block_rows)), STATE (len < 1, or
  * ipot_enable_blocks was not called), CUDA.
  */

@@ -55,6 +55,8 @@ chunk_fma_kernel(const __grid_constant__ ChunkParams p, int units)
     if (row0 >= n * G) return;   // (the whole cluster)
     const int rows = min(BM, n * G - row0), all_keys = p.len + (row0 + rows - 1) / G + 1, tiles = (all_keys + kCfKeys - 1) / kCfKeys;
     const int first = (int)((long long)tiles * rank / ranks) * kCfKeys, keys = min(all_keys, (int)((long long)tiles * (rank + 1) / ranks) * kCfKeys);
+    // weights enter the product with the values times this power of two: however many keys there are, their sum is at most 1, and no sum on the way is larger than the largest value
+    const float share = __int_as_float((127 - (32 - __clz(all_keys))) << 23);
     const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15, vecs = p.d / VE;
     const T *potK = (const T *)p.potK + (size_t)(p.unit0 + unit) * p.unit_rows * p.d, *potV = (const T *)p.potV + (size_t)(p.unit0 + unit) * p.unit_rows * p.d;
     const T *newK = (const T *)p.k + l * p.ks.layer + b * p.ks.stream + hkv * p.ks.head, *newV = (const T *)p.v + l * p.vs.layer + b * p.vs.stream + hkv * p.vs.head;
@@ -156,7 +158,7 @@ chunk_fma_kernel(const __grid_constant__ ChunkParams p, int units)
             for (int j = 0; j < 4; ++j) {
                 s[i][j] = chunk_ex2(s[i][j] - ref);
                 ps += s[i][j];
-                sm.p[ty + RS * i][tx + 16 * j] = s[i][j];
+                sm.p[ty + RS * i][tx + 16 * j] = s[i][j] * share;
             }
             m[i] = mn;
             sum[i] = sum[i] * corr + ps;   // this thread's share
@@ -201,7 +203,7 @@ chunk_fma_kernel(const __grid_constant__ ChunkParams p, int units)
             const int r = ty + RS * i, t = (row0 + r) / G, g = row0 + r - t * G;
             if (r >= rows) continue;
             T *o = out + g * p.os.head + (long long)t * p.os.token;
-            const float inv = 1.f / sum[i];
+            const float inv = 1.f / (sum[i] * share);
 #pragma unroll
             for (int c = 0; c < CV; ++c) {
                 struct alignas(4 * sizeof(T)) Four {
@@ -243,7 +245,7 @@ chunk_fma_kernel(const __grid_constant__ ChunkParams p, int units)
         }
         T *dst = out + g * p.os.head + (long long)t * p.os.token + 4 * c;
 #pragma unroll
-        for (int x = 0; x < 4; ++x) dst[x] = from_float<T>(o[x] / den);
+        for (int x = 0; x < 4; ++x) dst[x] = from_float<T>(o[x] / (den * share));
         if (c == 0 && p.lse) p.lse[(lse0 + g) * p.n + t] = 0.6931471805599453f * (ref + log2f(den));
     }
     cluster_sync();   // no block ends while others read its results

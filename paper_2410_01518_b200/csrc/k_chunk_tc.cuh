@@ -4,10 +4,10 @@
 // rows of floor(128 / G) tokens (TMA fetches it as a box of G heads x tokens, whatever the strides).  Keys come in tiles of KT,
 // first the pot's, then the chunk's.  Per tile and stream
 //   S = Q K^T   128 x KT fp32 in tensor memory (both operands in shared memory, K-major, 128-byte swizzle)
-//   softmax     a thread owns half of a row (one warp per scheduler and stream would be a chain of latencies: 1900 cycles a tile, two 1000): p = 2^(s c - m),
+//   softmax     a thread owns half of a row (one warp per scheduler and stream would be a chain of latencies: 1900 cycles a tile, two 1000): p = 2^(s c - m - 40),
 //               l += p in fp32, and p as bf16 over S in tensor memory.  No maximum is taken: fp32 and bf16 have the same exponents, so p is as exact far above 1
 //               as below.  The reference m is 0 unless the sum of the row's first tile is far from 1, and only a later tile whose sum passes 2^24 moves it (the row's sums and output
-//               are then scaled down).  Tiles with columns that some row does not see, those two kinds, and those of a row whose reference is beyond 2^24, take a general form that does take the maximum.  All exponentials are the
+//               are then scaled down).  The 40 orders are what a row's weights can sum up to so: all p together stay below 1, and no sum of p v on the way is larger than the largest value.  Tiles with columns that some row does not see, those two kinds, and those of a row whose reference is beyond 2^24, take a general form that does take the maximum.  All exponentials are the
 //               special-function unit's: a quarter of them as a polynomial on the FMA pipe took 1016 us for 4 streams x 2048 tokens over 6144 rows instead of 950
 //               (in long runs the power limit holds the clock at 1.6 GHz, and what is issued costs power).
 //   O += P V    P from tensor memory, V as it lies (channels contiguous: the N-major operand layout), 128 x D fp32 in tensor memory
@@ -33,10 +33,13 @@ namespace ipotk {
 
 constexpr int kCtRows = 128;
 constexpr unsigned long long kChunkLandNs = 200ull * 1000 * 1000;
-constexpr float kChunkMost = 16777216.f;   // 2^24: a tile's sum of a row up to here leaves the reference where it is (and 2^100 of fp32's range to the values)
-constexpr float kChunkLeast = 5.9604645e-8f;  // 2^-24: a first tile's sum from here on lets the reference be 0
+// Half a tile's sum of a row up to 2^24 leaves the reference where it is, and half a first tile's from 2^-12 on lets it be 0; both carry 2^-lift like all p.  2^40: two halves of up to 2^15
+// tiles.  (At the other end a product with a value keeps bf16's bits above 2^-117, so values below 2^-65 may begin to lose some.)
+constexpr float kChunkLift = 40.f, kChunkLifted = 1099511627776.f;   // and 2^40
+constexpr float kChunkMost = 1.52587890625e-05f;                     // 2^24 2^-40
+constexpr float kChunkLeast = 2.220446049250313e-16f;                // 2^-12 2^-40
 // A reference is a rounded product, and s c, not rounded before the reference is subtracted, misses it by up to half its last place: 1 and more from 2^24 on, further out more than the
-// exponential's range.  The general form rounds the product, so that the row's maximum comes out as exactly 0; near 0 that is as good.  From here on a row takes nothing else: its reference
+// exponential's range.  The general form rounds the product, so that the row's maximum comes out as exactly 0; near 0 that is as good.  References up to here are whole numbers, which add up exactly.  From here on a row takes nothing but the general form: its reference
 // then waits in its threads' shared memory and is NaN in their registers, so that a plain tile's sum is NaN and the check that there is fails.  (4 streams x 2048 tokens over 6144 rows
 // 953.4 -> 954.4 us, 2048 tokens into an empty pot 45.0 -> 45.6; a compare per tile and a flag across them cost 4.5 %.)
 constexpr float kChunkFar = 16777216.f;       // 2^24
@@ -130,12 +133,13 @@ __device__ __forceinline__ bool chunk_pair_any(int id, bool x)
 // A tile of a warp's rows in general: one with columns that some row does not see, a first one whose sum is far from 1, one that left the range, and every one of a row with a far
 // reference: the row's maximum becomes the reference if it is above it.
 // W columns from ts on, of which this row sees `cols`; the other warp of the pair has the other half and takes part.  seen: the row's two maxima and, between two tiles, a far reference, each
-// thread's in its half.  scale: whether O holds something already (W2 columns of it from `to` on are this warp's).  Leaves p over the first half of its columns; (reference or NaN, sum).
+// thread's in its half.  scale: whether O holds something already (W2 columns of it from `to` on are this warp's).  m: the reference + kChunkLift, as a plain tile takes it (-inf: none yet).
+// Leaves p over the first half of its columns; (reference + kChunkLift or NaN, sum).
 template <int W, int W2>
 __device__ __noinline__ float2 chunk_tile_general(uint32_t ts, uint32_t to, int cols, float c, float m, float sum, bool valid, bool scale, float2 *seen, int half, int pair)
 {
     float *mine = half ? &seen->y : &seen->x;
-    if (isnan(m)) m = *mine;
+    m = isnan(m) ? *mine : m - kChunkLift;
     uint32_t v[W / 32][32];
     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
@@ -152,7 +156,7 @@ __device__ __noinline__ float2 chunk_tile_general(uint32_t ts, uint32_t to, int 
     float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
     *mine = top;
     chunk_pair_sync(pair);
-    top = fmaxf(seen->x, seen->y) * c;
+    top = ceilf(fmaxf(seen->x, seen->y) * c);
     const bool moves = valid && top > m;
     if (__any_sync(0xffffffffu, moves)) {   // (the same rows, the same answer in both warps)
         const float to_m = moves ? top : m, f = moves ? chunk_ex2(m - to_m) : 1.f;   // (m = -inf: 0)
@@ -172,13 +176,15 @@ __device__ __noinline__ float2 chunk_tile_general(uint32_t ts, uint32_t to, int 
         }
     }
     const float ref = m == -INFINITY ? 0.f : m;
+    const float2 r2 = make_float2(-ref, -ref), l2 = make_float2(-kChunkLift, -kChunkLift);
     float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int a = 0; a < W / 32; ++a) {
         uint32_t h[16];
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
-            const float x = chunk_ex2(__fmul_rn(__uint_as_float(v[a][e]), c) - ref), y = chunk_ex2(__fmul_rn(__uint_as_float(v[a][e + 1]), c) - ref);   // (-inf: 0)
+            const float2 z = __fadd2_rn(__fadd2_rn(make_float2(__fmul_rn(__uint_as_float(v[a][e]), c), __fmul_rn(__uint_as_float(v[a][e + 1]), c)), r2), l2);
+            const float x = chunk_ex2(z.x), y = chunk_ex2(z.y);   // (-inf: 0)
             s[e & 2] += x;
             s[(e & 2) + 1] += y;
             const __nv_bfloat162 b = __floats2bfloat162_rn(x, y);
@@ -190,6 +196,8 @@ __device__ __noinline__ float2 chunk_tile_general(uint32_t ts, uint32_t to, int 
     if (fabsf(ref) >= kChunkFar) {
         *mine = m;
         m = NAN;
+    } else {
+        m += kChunkLift;
     }
     return make_float2(m, sum + ((s[0] + s[1]) + (s[2] + s[3])));
 }
@@ -391,7 +399,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
         const int mine = tiles <= 0 || tokens[qt] <= 0 ? 0 : kSplit ? (tiles - i + S - 1) / S : tiles;
         const float c = p.c.scale_log2e;
         float2 *stat = reinterpret_cast<float2 *>(ct_raw + L::kOffStat) + i * kCtRows + row;   // (what the row's two threads tell each other; at the end its statistics)
-        float m = -INFINITY, sum = 0.f;   // the sum is this half's
+        float m = -INFINITY, sum = 0.f;   // the reference + kChunkLift; the sum is this half's
         for (int j = 0; j < mine; ++j) {
             const int tile = first + (kSplit ? j * S + i : j);
             // columns that this row sees
@@ -404,7 +412,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                 bool general = masked;
                 if (!general) {
                     uint32_t h[W / 32][16];
-                    const float ref = j ? m : 0.f, s = chunk_tile<W>(ts, c, ref, h);
+                    const float ref = j ? m : kChunkLift, s = chunk_tile<W>(ts, c, ref, h);
                     general = chunk_pair_any(pair, valid && !(s < kChunkMost && (j || s > kChunkLeast)));   // (the logits are still there)
                     if (!general) {
                         m = ref;
@@ -430,7 +438,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
             tc_fence_after();
         }
         if (works) {   // the two halves' sums
-            if (isnan(m)) m = half ? stat->y : stat->x;   // (a far reference)
+            m = isnan(m) ? (half ? stat->y : stat->x) : m - kChunkLift;   // (NaN: a far reference)
             (half ? stat->y : stat->x) = sum;
             chunk_pair_sync(pair);
             sum = stat->x + stat->y;
@@ -456,7 +464,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                     if (valid && W2 * half + a + e < p.c.d) *reinterpret_cast<uint4 *>(o + a + e) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
-            if (valid && !half && p.c.lse) p.c.lse[(((size_t)l * p.c.streams + b) * p.c.Hkv * G + hkv * G + g) * p.c.n + t] = 0.6931471805599453f * (m + log2f(sum));
+            if (valid && !half && p.c.lse) p.c.lse[(((size_t)l * p.c.streams + b) * p.c.Hkv * G + hkv * G + g) * p.c.n + t] = 0.6931471805599453f * (m + log2f(sum * kChunkLifted));
         }
     }
     if (kSplit) {
@@ -519,7 +527,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
             if (ranks > 1) {
                 if (!half) stat[row] = make_float2(ref, den);   // (everyone has read what was there)
             } else if (valid && !half && p.c.lse) {
-                p.c.lse[(((size_t)l * p.c.streams + b) * p.c.Hkv * G + hkv * G + g) * p.c.n + t] = 0.6931471805599453f * (ref + log2f(den));
+                p.c.lse[(((size_t)l * p.c.streams + b) * p.c.Hkv * G + hkv * G + g) * p.c.n + t] = 0.6931471805599453f * (ref + log2f(den * kChunkLifted));
             }
         }
         if (ranks > 1) {
@@ -583,7 +591,7 @@ chunk_tc_kernel(const __grid_constant__ CUtensorMap mapQ, const __grid_constant_
                 const int ti = row / G, g = row - ti * G, t = t0 + ti;
                 __nv_bfloat16 *out = (__nv_bfloat16 *)p.c.out + l * p.c.os.layer + b * p.c.os.stream + (long long)(hkv * G + g) * p.c.os.head + (long long)t * p.c.os.token;
                 *reinterpret_cast<uint4 *>(out + 8 * v) = make_uint4(w[0], w[1], w[2], w[3]);
-                if (v == 0 && p.c.lse) p.c.lse[(((size_t)l * p.c.streams + b) * p.c.Hkv * G + hkv * G + g) * p.c.n + t] = 0.6931471805599453f * (ref + log2f(den));
+                if (v == 0 && p.c.lse) p.c.lse[(((size_t)l * p.c.streams + b) * p.c.Hkv * G + hkv * G + g) * p.c.n + t] = 0.6931471805599453f * (ref + log2f(den * kChunkLifted));
             }
             cluster_sync();   // no block ends while others read or send
         }

@@ -33,6 +33,10 @@ __device__ __forceinline__ float few_ex2(float x)
 // 2^(m - ref), 0 where nothing has been seen (m = -inf) whatever ref is
 __device__ __forceinline__ float few_scale(float m, float ref) { return m == -INFINITY ? 0.f : few_ex2(m - ref); }
 
+// Weights enter the product with the values times this: at most 2^15 slots and 16 tokens of weights up to 1 then sum up to at most 1, and no sum on the way is larger than the largest value.
+// (A power of two: nothing is rounded by it, down to values of 2^-80.)
+constexpr float kFewShare = 1.f / 65536.f;
+
 constexpr int kFewThreads = 128, kFewWarps = kFewThreads / 32, kFewMaxRanks = kMostRanks;
 constexpr int kFewRows = 8;       // query rows of a block
 constexpr int kFewBlocks = 2048;  // blocks of a unit: 32768 slots, 16 rows
@@ -304,7 +308,7 @@ __device__ __forceinline__ int select_blocks(FewShared &sh, uint8_t *free_bytes,
 }
 
 // ------------------------------------------------------------------ the end of a block's work
-// part: [warps][rows][d + 4] outputs against the references in sh.warp_stat; got: room for the blocks' shares of the result.
+// part: [warps][rows][d + 4] outputs against the references in sh.warp_stat, times kFewShare; got: room for the blocks' shares of the result.
 // kAlone: with a way of its own for a block that is its own cluster, which has much for few threads (selected blocks of 256 units 38.4 -> 36.6 us).  Its code costs launches of few
 // units, which never come there, 0.6 of 7.3 us: a single token's few microseconds are worth more than 2 of the 80 that many units take.
 template <typename O, bool kAlone>
@@ -342,14 +346,15 @@ __device__ __forceinline__ void few_finish(float *part, float *got, FewShared &s
         for (int e = threadIdx.x * 4; e < all; e += kFewThreads * 4) {
             const int h = e / p.d, c = e - h * p.d, t = (u.row0 + h) / p.G, g = u.hkv * p.G + u.row0 + h - t * p.G;
             const float2 st = sh.stat[0][h];
+            const float den = st.y * kFewShare;
             const float4 x = *reinterpret_cast<const float4 *>(got + e);
             struct alignas(4 * sizeof(O)) Four {
                 O e[4];
             } out;
-            out.e[0] = from_float<O>(x.x / st.y);
-            out.e[1] = from_float<O>(x.y / st.y);
-            out.e[2] = from_float<O>(x.z / st.y);
-            out.e[3] = from_float<O>(x.w / st.y);
+            out.e[0] = from_float<O>(x.x / den);
+            out.e[1] = from_float<O>(x.y / den);
+            out.e[2] = from_float<O>(x.z / den);
+            out.e[3] = from_float<O>(x.w / den);
             *reinterpret_cast<Four *>((O *)p.out + u.l * p.os.layer + u.b * p.os.stream + g * p.os.head + (long long)t * p.os.token + c) = out;
             if (c == 0 && p.lse) p.lse[(((size_t)u.l * p.streams + u.b) * p.Hkv * p.G + g) * p.n + t] = 0.6931471805599453f * (st.x + log2f(st.y));
         }
@@ -379,7 +384,7 @@ __device__ __forceinline__ void few_finish(float *part, float *got, FewShared &s
             sum = fmaf(st[r].y, f, sum);
         }
         const int t = (u.row0 + h) / p.G, g = u.hkv * p.G + u.row0 + h - t * p.G;
-        ((O *)p.out)[u.l * p.os.layer + u.b * p.os.stream + g * p.os.head + (long long)t * p.os.token + c] = from_float<O>(o / sum);
+        ((O *)p.out)[u.l * p.os.layer + u.b * p.os.stream + g * p.os.head + (long long)t * p.os.token + c] = from_float<O>(o / (sum * kFewShare));
         if (c == 0 && p.lse) p.lse[(((size_t)u.l * p.streams + u.b) * p.Hkv * p.G + g) * p.n + t] = 0.6931471805599453f * (ref + log2f(sum));
     }
 }
@@ -572,6 +577,7 @@ few_mma_kernel(const __grid_constant__ FewParams p)
         for (int j = 0; j < 4; ++j) {
             w[j] = few_ex2(sc[j] - m);   // -inf -> 0
             l += w[j];
+            w[j] *= kFewShare;
         }
         // A fragments of the weights (columns: the tile's keys); kSparse: the first two of three terms in rows 0 .. 7 and 8 .. 15, then the third
         const uint32_t a0 = few_pack(w[0], w[1]), a2 = few_pack(w[2], w[3]);
@@ -737,8 +743,9 @@ few_fma_kernel(const __grid_constant__ FewParams p, int lpk)
             }
 #pragma unroll
             for (int j = 0; j < KT; ++j) {
-                const float w = h >= seen_by[j] ? few_ex2(s[j][h] - mn) : 0.f;
+                float w = h >= seen_by[j] ? few_ex2(s[j][h] - mn) : 0.f;
                 l[h] += w;
+                w *= kFewShare;
 #pragma unroll
                 for (int x = 0; x < VPL; ++x) {
                     acc[h][x].x = fmaf(w, vv[j][x].x, acc[h][x].x);
