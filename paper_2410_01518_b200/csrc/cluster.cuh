@@ -1,6 +1,7 @@
 // Thread-block clusters: their blocks' shared memory, and launches.
 #pragma once
 #include <atomic>
+#include <cstdint>
 
 #include "common.cuh"
 
@@ -80,7 +81,9 @@ inline void cluster_config(cudaLaunchConfig_t &lc, cudaLaunchAttribute (&at)[2],
     lc.numAttrs = 2;
 }
 
-// A launch of clusters along x, as a programmatic dependent like launch_pdl's.
+// A launch of clusters along x, as a programmatic dependent like launch_pdl's.  More than 8 blocks a cluster (not portable, but this part has 16) have to be allowed to a kernel on
+// every device that it runs on, and anew after a device's reset: at each launch, like the size of its shared memory.
+constexpr int kPortableRanks = 8;
 template <typename... P, typename... A>
 inline cudaError_t launch_cluster(void (*kern)(P...), dim3 grid, dim3 block, size_t smem, int cluster, cudaStream_t stream, const A &...args)
 {
@@ -88,30 +91,43 @@ inline cudaError_t launch_cluster(void (*kern)(P...), dim3 grid, dim3 block, siz
     cudaLaunchAttribute at[2];
     cluster_config(lc, at, grid, block, smem, cluster);
     lc.stream = stream;
+    if (cluster > kPortableRanks) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e != cudaSuccess) return e;
+    }
     return cudaLaunchKernelEx(&lc, kern, P(args)...);
 }
 
 // Blocks of a cluster for `items` pieces of work, each spread over one: the most, up to `most`, with which all clusters run side by side.  How many do is the driver's answer, asked once
-// per kernel and size: the blocks of a cluster share a GPC, and with one block an SM 15 clusters of 8 fit this part, not 18.  (More than 8 blocks are not portable, but it has 16.)
+// per kernel, device, shared memory of a block and size: the blocks of a cluster share a GPC, and with one block an SM 15 clusters of 8 fit this part, not 18.
 constexpr int kMostRanks = 16;
-struct ClusterFit {
-    std::atomic<int> fits[kMostRanks + 1];   // 0: not asked yet
+struct ClusterFit {   // of one kernel
+    static constexpr int kDevices = 16, kSizes = 8;   // (beyond these, or where two sizes share a place, it is asked again)
+    std::atomic<uint64_t> seen[kDevices][kSizes][kMostRanks + 1];   // shared memory << 32 | clusters + 1; 0: not asked yet
 };
 template <typename Kernel>
 inline int choose_cluster(ClusterFit &fit, Kernel kern, dim3 block, size_t smem, long long items, int most)
 {
+    int device;
+    if (cudaGetDevice(&device) != cudaSuccess) {
+        cudaGetLastError();
+        return 1;
+    }
+    const uint32_t size = (uint32_t)smem * 2654435761u >> 29;
     for (int c = most < kMostRanks ? most : kMostRanks; c > 1; --c) {
-        int n = fit.fits[c].load(std::memory_order_relaxed);
-        if (!n) {
+        std::atomic<uint64_t> *place = device < ClusterFit::kDevices ? &fit.seen[device][size][c] : nullptr;
+        const uint64_t was = place ? place->load(std::memory_order_relaxed) : 0;
+        int n = (int)(was & 0xffffffffu) - 1;
+        if (!was || was >> 32 != smem) {
             cudaLaunchConfig_t lc = {};
             cudaLaunchAttribute at[2];
             cluster_config(lc, at, dim3(c), block, smem, c);
-            if ((c > 8 && cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) || cudaOccupancyMaxActiveClusters(&n, kern, &lc) != cudaSuccess) {
+            if ((c > kPortableRanks && cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) ||
+                cudaOccupancyMaxActiveClusters(&n, kern, &lc) != cudaSuccess) {
                 cudaGetLastError();
                 n = 0;
             }
-            if (n < 1) n = -1;   // (none)
-            fit.fits[c].store(n, std::memory_order_relaxed);
+            if (place) place->store((uint64_t)smem << 32 | (uint32_t)(n + 1), std::memory_order_relaxed);
         }
         if (items <= n) return c;
     }
