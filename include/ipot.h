@@ -318,7 +318,8 @@ int ipot_view_rope(ipot_t *pot, void **K_rot);
  *                        times divided by s, between the two a blend that is linear in the number of turns
  *   IPOT_ROPE_RAMP       a blend that is linear in i: t_i up to pair floor(D(high)), t_i / s from pair ceil(D(low)) on, where
  *                        D(b) = r ln(L / (2 pi b)) / (2 ln base) is the pair that turns b times in L positions
- *                        (both limited to 0 .. r - 1).  Its magnitude, where 0 is given, is 0.1 ln(s) + 1; of all others 1.
+ *                        (both limited to 0 .. r - 1).  Its magnitude, where 0 is given, is 0.1 ln(s) + 1 for s > 1 and 1 otherwise; of
+ *                        all others 1.
  * Angles are taken in 64 bits and reduced there; cosine and sine are fp32, rounded once to the table's type.
  *   cos_table, sin_table : device, [n][rotary_dim / 2] of type dtype (IPOT_BF16 or IPOT_F32), 16-byte aligned
  *   cuda_stream          : cudaStream_t of the current device (NULL = the default stream); the call only queues work

@@ -645,7 +645,7 @@ bool rope_turns(const ipot_rope_spec_t &c, RopeTableParams &p)
         p.turns[i] = (keep == 1.0 ? t : keep == 0.0 ? t / s : t * keep + t / s * (1.0 - keep)) / (2.0 * pi);
     }
     p.half = r / 2;
-    p.magnitude = (float)(c.magnitude > 0.0 ? c.magnitude : c.scaling == IPOT_ROPE_RAMP ? 0.1 * std::log(s) + 1.0 : 1.0);
+    p.magnitude = (float)(c.magnitude > 0.0 ? c.magnitude : c.scaling == IPOT_ROPE_RAMP && s > 1.0 ? 0.1 * std::log(s) + 1.0 : 1.0);
     return true;
 }
 }  // namespace
