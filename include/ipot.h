@@ -324,7 +324,7 @@ int ipot_view_rope(ipot_t *pot, void **K_rot);
  *   cos_table, sin_table : device, [n][rotary_dim / 2] of type dtype (IPOT_BF16 or IPOT_F32), 16-byte aligned
  *   cuda_stream          : cudaStream_t of the current device (NULL = the default stream); the call only queues work
  * No pot is involved.  Errors: INVALID (NULL, misaligned; rotary_dim odd, < 2 or > 256; n < 1; first < 0 or first + n > 2^31;
- * base <= 1, factor <= 0, magnitude < 0 or one of them not finite; BANDS and RAMP: L <= 0, low <= 0 or high <= low; STRETCHED:
+ * base <= 1, factor <= 0, magnitude < 0 or one of them not finite; a magnitude beyond fp32 or angles beyond 64 bits; BANDS and RAMP: L <= 0, low <= 0 or high <= low; STRETCHED:
  * rotary_dim 2), CUDA.
  */
 enum {

@@ -3,6 +3,7 @@
 #include "../../include/ipot.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdio>
 #include <cstdlib>
@@ -643,8 +644,10 @@ bool rope_turns(const ipot_rope_spec_t &c, RopeTableParams &p)
         else if (c.scaling == IPOT_ROPE_BANDS) keep = std::min(1.0, std::max(0.0, (L * t / (2.0 * pi) - c.low) / (c.high - c.low)));
         else if (c.scaling == IPOT_ROPE_RAMP) keep = 1.0 - std::min(1.0, std::max(0.0, (i - lo) / std::max(hi - lo, 0.001)));
         p.turns[i] = (keep == 1.0 ? t : keep == 0.0 ? t / s : t * keep + t / s * (1.0 - keep)) / (2.0 * pi);
+        if (!std::isfinite(p.turns[i] * (double)(1LL << 31))) return false;   // (the largest position)
     }
     p.half = r / 2;
+    if (c.magnitude > FLT_MAX) return false;
     p.magnitude = (float)(c.magnitude > 0.0 ? c.magnitude : c.scaling == IPOT_ROPE_RAMP && s > 1.0 ? 0.1 * std::log(s) + 1.0 : 1.0);
     return true;
 }

@@ -1,4 +1,5 @@
 """Rotary tables (ipot_rope_tables) at the ends of their parameters' ranges; definitions and tolerances are those of test_rotary_gpu.py."""
+import ctypes as C
 import math
 
 import numpy as np
@@ -26,3 +27,16 @@ def test_a_ramp_that_does_not_stretch_has_magnitude_one(factor, dtype):
         # the frequency itself is off by a few 2^-53 (pow, the division by 2 pi, the blend); 2^-50 of the angle covers them and the product
         bound = mag * (2.0 ** -50 * ang.astype(np.float64) + math.pi * 2.0 ** -25 + 2.0 ** -23 + 2.0 ** -24) + half_step * np.abs(w) + 2.0 ** -130
         assert (np.abs(g - w) <= bound).all(), float(np.max(np.abs(g - w) / bound))
+
+
+def test_tables_without_numbers_are_refused():
+    """Angles or magnitudes that no longer are numbers; found on the host, no device needed."""
+    L = ipot.lib()
+
+    def rc(scaling, factor=2.0, base=1e4, mag=0.0, rotary=64, original=4096.0):
+        s = ipot.ipot_rope_spec_t(rotary, scaling, base, factor, original, 1.0, 4.0, mag)
+        return L.ipot_rope_tables(C.byref(s), 0, 8, ipot.IPOT_F32, 4096, 4096 << 8, None)
+
+    for kw in (dict(scaling=ipot.IPOT_ROPE_LINEAR, factor=1e-307), dict(scaling=ipot.IPOT_ROPE_BANDS, factor=1e-307), dict(scaling=ipot.IPOT_ROPE_RAMP, factor=1e-307, original=1e-300),
+               dict(scaling=ipot.IPOT_ROPE_LINEAR, factor=5e-324), dict(scaling=ipot.IPOT_ROPE_PLAIN, mag=3.5e38), dict(scaling=ipot.IPOT_ROPE_PLAIN, mag=1e300)):
+        assert rc(**kw) == ipot.IPOT_E_INVALID, kw
