@@ -32,7 +32,7 @@ struct ipot {
     ipot_config_t cfg;
     int len;
     int device;
-    int sm_count;
+    int sm_count, l2_bytes;
     int scorer;
     int G, units, elem_bytes, row_bytes;
     cudaStream_t stream;
@@ -733,7 +733,8 @@ int ipot_create_ex(const ipot_config_t *cfg, ipot_t **out)
     p->scorer = IPOT_SCORER_AUTO;
     p->withhold_chunk = -1;
     if (cudaGetDevice(&p->device) != cudaSuccess ||
-        cudaDeviceGetAttribute(&p->sm_count, cudaDevAttrMultiProcessorCount, p->device) != cudaSuccess) {
+        cudaDeviceGetAttribute(&p->sm_count, cudaDevAttrMultiProcessorCount, p->device) != cudaSuccess ||
+        cudaDeviceGetAttribute(&p->l2_bytes, cudaDevAttrL2CacheSize, p->device) != cudaSuccess) {
         cudaGetLastError();
         delete p;
         return IPOT_E_CUDA;
@@ -1181,7 +1182,7 @@ int ipot_chunk_attention(ipot_t *p, int layer, int n_layers, int n, const int32_
     c.layers = n_layers; c.streams = p->cfg.batch; c.Hkv = p->cfg.Hkv; c.G = p->G; c.d = p->cfg.d; c.n = n;
     c.scale_log2e = (float)(1.4426950408889634 / std::sqrt((double)p->cfg.d));
     c.status = p->status;
-    const ChunkTcHost host{(void *)p->tc.encode, p->sm_count, p->units, p->ts.withhold_rank, p->ts.wait_ns};
+    const ChunkTcHost host{(void *)p->tc.encode, p->sm_count, p->l2_bytes, p->units, p->ts.withhold_rank, p->ts.wait_ns};
     IPOT_CUDA(launch_chunk_attention(c, p->cfg.dtype == IPOT_F32, host, p->stream));
     p->launches += 1;
     return IPOT_OK;

@@ -27,16 +27,31 @@ cudaError_t launch_rope_rows(const RopeRowsParams &p, bool f32, bool table_f32, 
     return interleaved ? launch_rope_rows_t<bf16, bf16, true>(p, stream) : launch_rope_rows_t<bf16, bf16, false>(p, stream);
 }
 
-// Few rows have a kernel of their own: up to 8 of a KV head, or two groups of 8 that each go over the keys, as long as the second finds them in L2 (bf16, 8 heads a
-// KV head of 128 channels, us, this / tcgen05: 16 rows, 8 units x 4095 keys 11.6 / 15.8, 64 units 33.5 / 35.1, 256 units 152 / 117; 8 units x 16000 25.6 / 27.0, 64 units 103 / 91).
+// Few rows have a kernel of their own: up to 8 of a KV head, or two groups of 8 that each go over the keys.
+// Two groups (us, this / the other kernel for 9 rows and more; 16 rows, units x keys).  bf16: as long as half of L2 holds the keys, so that the second group finds what the first has read, and
+// the groups do not queue for SMs (a block's shared memory goes with d); or where a handful of units leaves the other kernel, 8 blocks a unit, most SMs idle.
+//   d = 64   16 x 2000 6.3/8.8   64 x 4095 20/21    128 x 2000 21/19   256 x 2000 40/53
+//   d = 128  4 x 32000 29/40   8 x 4095 14/15   8 x 16000 28/25   32 x 2000 12/15   32 x 16000 57/52   64 x 500 10/12   64 x 8000 57/53   128 x 500 17/12   256 x 4095 153/116
+//   d = 256  2 x 32000 46/86   8 x 2000 15/15   8 x 16000 56/49   16 x 1000 1.10   24 x 1000 0.80   32 x 500 15/13   256 x 4095 366/181
+// f32, where the other kernel has more to issue: by the groups alone.
+//   d = 64   8 x 32000 220/360   32 x 4095 76/87   64 x 8000 293/294   96 x 2000 1.33   128 x 2000 222/150
+//   d = 128  2 x 32000 331/598   8 x 4095 56/91    48 x 2000 1.29      96 x 2000 1.36   128 x 2000 453/306
+//   d = 256  8 x 4095 102/167   16 x 2000 1.43   24 x 2000 0.89   32 x 4095 345/309
+// (Over 521 calls of 1 to 256 units, 32 to 256 channels and 300 to 32000 keys the choice costs 1.4 % on average, up to 45 % at 256 units x 64 channels.)
 // Else tensor cores for bf16, unless a group's heads do not fit into one tile of query rows or the strides are none that a tensor map
 // takes (an input whose rows repeat by a stride of 0).
+static bool two_groups_of_rows(const ChunkParams &p, bool f32, long long l2_bytes)
+{
+    const long long units = (long long)p.layers * p.streams * p.Hkv;
+    if (f32) return units <= (p.d <= 128 ? 96 : 16);
+    const double key_bytes = 4.0 * units * ((double)p.len + p.n) * p.d;
+    return units <= 4 || (key_bytes <= 0.5 * l2_bytes && units * p.d <= (p.d <= 128 ? 8192 : 4096));
+}
+
 cudaError_t launch_chunk_attention(const ChunkParams &p, bool f32, const ChunkTcHost &host, cudaStream_t stream)
 {
-    constexpr double kStaysInL2 = 134e6;
     const int rows = p.n * p.G;   // (at most 2^30)
-    const double key_bytes = 2.0 * p.layers * p.streams * p.Hkv * ((double)p.len + p.n) * p.d * (f32 ? 4 : 2);
-    if (rows <= kFewRows || (rows <= 2 * kFewRows && key_bytes <= kStaysInL2)) {
+    if (rows <= kFewRows || (rows <= 2 * kFewRows && two_groups_of_rows(p, f32, host.l2_bytes))) {
         FewParams f = {};
         f.q = p.q; f.qs = p.qs; f.K = p.potK; f.V = p.potV;
         f.unit0 = p.unit0; f.unit_rows = p.unit_rows; f.len = p.len;

@@ -50,10 +50,10 @@ struct ChunkParams {
     float scale_log2e;
     int *status;
 };
-// What the tensor-core kernel needs besides.
+// What the choice of a kernel and the tensor-core kernel need besides.
 struct ChunkTcHost {
     void *encode;                  // cuTensorMapEncodeTiled, or NULL: no tensor-core kernel
-    int sm_count, pot_units;
+    int sm_count, l2_bytes, pot_units;
     int withhold;                  // -1; test hook: this stream's softmax never reports
     unsigned long long wait_ns;
 };
