@@ -661,11 +661,13 @@ inline cudaError_t launch_chunk_tc(const ChunkParams &c, const ChunkTcHost &host
 {
     const int tile_tokens = kCtRows / c.G, tiles = (c.n + tile_tokens - 1) / tile_tokens;
     const long long units = (long long)c.layers * c.streams * c.Hkv;
-    // Two query tiles a block share its key tiles where one tile a block would need more than a round of blocks (us, two / one: 2 x 3 streams x 333 tokens over 1999 rows, 4 KV
-    // heads 44 / 53; 1024 over 2048, 8 KV heads 53 / 61; 2 x 512 over 4096 74 / 90).  Streams of different lengths: how long the host does not know; a quarter of the tiles
-    // is taken to be padding (the first of these with 333, 222 and 111 tokens: 43 / 30).
-    const long long all = units * tiles;
-    const bool pairs = c.d <= 128 && (c.tokens ? all - all / 4 : all) > host.sm_count;
+    // Two query tiles a block share its key tiles, in half as many blocks that each take 1.45 times as long (two streams per key tile are then both busy); one goes faster where that saves no
+    // round of blocks.  us, two / one: 12 units of 12 tiles over 2000 rows 43 / 30, 13 tiles 44 / 51, 22 tiles 49 / 58, 25 tiles 80 / 83; 32 units of 9 tiles 77 / 56, 10 tiles 80 / 83.
+    // Streams of different lengths: how long the host does not know; a quarter of the tiles is taken to be padding.  3 streams of 180 tiles, with no padding, 15, 25 and 50 % of it: 46 / 54,
+    // 45 / 52, 45 / 31, 44 / 30.  (Full streams lose a sixth by it between 149 and 197 tiles, padded ones gain a third; over 90 calls of 2 to 8 streams with 0 to 50 % padding and 150 to 350
+    // tiles the choice costs 5 % on average, and without the quarter 12 %.)
+    auto rounds = [&](long long blocks) { return ((c.tokens ? blocks - blocks / 4 : blocks) + host.sm_count - 1) / host.sm_count; };
+    const bool pairs = c.d <= 128 && 4 * rounds(units * ((tiles + 1) / 2)) < 3 * rounds(units * tiles);
     if (c.d > 128) return launch_chunk_tc_t<256, true>(c, host, tile_tokens, tiles, stream, done);
     if (c.d > 64) return pairs ? launch_chunk_tc_t<128, false>(c, host, tile_tokens, tiles, stream, done)
                                : launch_chunk_tc_t<128, true>(c, host, tile_tokens, tiles, stream, done);
