@@ -30,14 +30,14 @@ cudaError_t launch_rope_rows(const RopeRowsParams &p, bool f32, bool table_f32, 
 // Few rows have a kernel of their own: up to 8 of a KV head, or two groups of 8 that each go over the keys.
 // Two groups (us, this / the other kernel for 9 rows and more; 16 rows, units x keys).  bf16: as long as half of L2 holds the keys, so that the second group finds what the first has read, and
 // the groups do not queue for SMs (a block's shared memory goes with d); or where a handful of units leaves the other kernel, 8 blocks a unit, most SMs idle.
-//   d = 64   16 x 2000 6.3/8.8   64 x 4095 20/21    128 x 2000 21/19   256 x 2000 40/53
-//   d = 128  4 x 32000 29/40   8 x 4095 14/15   8 x 16000 28/25   32 x 2000 12/15   32 x 16000 57/52   64 x 500 10/12   64 x 8000 57/53   128 x 500 17/12   256 x 4095 153/116
+//   d = 64   16 x 2000 6.3/8.8   64 x 4095 20/21    128 x 2000 21/19   256 x 2000 40/38
+//   d = 128  4 x 32000 29/40   8 x 4095 14/15   8 x 16000 28/25   32 x 2000 12/15   32 x 16000 57/52   64 x 500 10/12   64 x 8000 57/53   128 x 500 17/12   256 x 4095 153/96
 //   d = 256  2 x 32000 46/86   8 x 2000 15/15   8 x 16000 56/49   16 x 1000 1.10   24 x 1000 0.80   32 x 500 15/13   256 x 4095 366/181
 // f32, where the other kernel has more to issue: by the groups alone.
 //   d = 64   8 x 32000 220/360   32 x 4095 76/87   64 x 8000 293/294   96 x 2000 1.33   128 x 2000 222/150
 //   d = 128  2 x 32000 331/598   8 x 4095 56/91    48 x 2000 1.29      96 x 2000 1.36   128 x 2000 453/306
 //   d = 256  8 x 4095 102/167   16 x 2000 1.43   24 x 2000 0.89   32 x 4095 345/309
-// (Over 521 calls of 1 to 256 units, 32 to 256 channels and 300 to 32000 keys the choice costs 1.4 % on average, up to 45 % at 256 units x 64 channels.)
+// (Over 493 calls of 1 to 256 units, 64 to 256 channels and 300 to 32000 keys the choice costs 1 % on average; most, 1.8 times, for f32 at 24 units x 300 keys x 256 channels.)
 // Else tensor cores for bf16, unless a group's heads do not fit into one tile of query rows or the strides are none that a tensor map
 // takes (an input whose rows repeat by a stride of 0).
 static bool two_groups_of_rows(const ChunkParams &p, bool f32, long long l2_bytes)
