@@ -344,6 +344,8 @@ def _plain_tables(c, s):
 
 def _own_state(c, s):
     """The pot that a program holds, filled, and views of what a call leaves in it."""
+    import sys
+
     from paper_2410_01518_b200 import ipot
 
     s.ipot = ipot
@@ -358,7 +360,7 @@ def _own_state(c, s):
                                          dtype=ipot.IPOT_F32 if c["dtype"] == "f32" else ipot.IPOT_BF16, nuc_slots=0, max_cap_rows=1)
 
         def __del__(self):
-            if self.h is not None:
+            if self.h is not None and not sys.is_finalizing():   # (at exit the binding is gone before the pots, and memory goes with the process)
                 ipot.ipot_destroy(self.h)
 
         def view(self, addr, shape, dtype):
