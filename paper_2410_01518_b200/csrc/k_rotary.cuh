@@ -112,11 +112,11 @@ struct RowHeads {
 
 // grid (blocks over tokens x items, head groups, layers x streams).  Items of a row: half pairing, one per vector of the lower
 // half (it brings its partner); interleaved, one per rotated vector; and one per vector, or two vectors, that are copied.  Both kinds load before
-// and store behind the rotation: a warp has items of both.  far: more is written than L2 holds until it is read; stores that do not stay there then leave the loads undisturbed
-// (16 streams x 2048 tokens x 40 heads x 128 channels, half of them rotated: 66.9 us -> 60.1, 5.94 TB/s).
+// and store behind the rotation: a warp has items of both.  16 streams x 2048 tokens x 40 heads x 128 channels (671 MB): 98.8 us, 6.8 TB/s, all or half of them rotated; streams of
+// different lengths, half as many rows, 60 us, 5.9 TB/s.  (Stored as a struct of elements: 138 us.  Stores that are evicted first: no gain out of place, 84 MB in place 20 -> 24 us.)
 template <typename T, typename TT, bool kInterleaved>
 __global__ void __launch_bounds__(kRotThreads)
-rope_rows_kernel(const __grid_constant__ RopeRowsParams p, int items, bool far)
+rope_rows_kernel(const __grid_constant__ RopeRowsParams p, int items)
 {
     pdl_wait();
     pdl_release();
@@ -163,22 +163,19 @@ rope_rows_kernel(const __grid_constant__ RopeRowsParams p, int items, bool far)
     }
 #pragma unroll
     for (int i = 0; i < kRowHeads; ++i)
-        if (i < rows.n) {
-            RowVec<T> *o = reinterpret_cast<RowVec<T> *>(dst + i * rows.out_head);
-            if (far) {
-                __stcs(reinterpret_cast<uint4 *>(o + v), *reinterpret_cast<const uint4 *>(x + i));
-                if (two) __stcs(reinterpret_cast<uint4 *>(o + v2), *reinterpret_cast<const uint4 *>(y + i));
-            } else {
-                o[v] = x[i];
-                if (two) o[v2] = y[i];
-            }
-        }
+        if (i < rows.n) reinterpret_cast<uint4 *>(dst + i * rows.out_head)[v] = *reinterpret_cast<const uint4 *>(x + i);
+    if (two) {
+#pragma unroll
+        for (int i = 0; i < kRowHeads; ++i)
+            if (i < rows.n) reinterpret_cast<uint4 *>(dst + i * rows.out_head)[v2] = *reinterpret_cast<const uint4 *>(y + i);
+    }
 }
 
-// Rotated parts that do not split into whole vectors: a thread has one channel pair, or one channel that is copied.
+// Rotated parts that do not split into whole vectors: a thread has one channel pair, or one channel that is copied.  Bound: 2-byte accesses (122 of 128 channels in the case above 295 us, 26 of
+// them 423).
 template <typename T, typename TT, bool kInterleaved>
 __global__ void __launch_bounds__(kRotThreads)
-rope_pairs_kernel(const __grid_constant__ RopeRowsParams p, int items, bool)
+rope_pairs_kernel(const __grid_constant__ RopeRowsParams p, int items)
 {
     pdl_wait();
     pdl_release();
@@ -221,8 +218,7 @@ inline cudaError_t launch_rope_rows_t(const RopeRowsParams &p, cudaStream_t stre
     const int groups = (p.heads[0] + kRowHeads - 1) / kRowHeads + (p.heads[1] + kRowHeads - 1) / kRowHeads;
     const long long threads = (long long)p.n * items;
     const dim3 grid((unsigned)((threads + kRotThreads - 1) / kRotThreads), groups, p.layers * p.streams);
-    const bool far = (double)p.layers * p.streams * (p.heads[0] + p.heads[1]) * p.n * p.d * sizeof(T) > 64e6;
-    return launch_pdl(vectors ? rope_rows_kernel<T, TT, kInterleaved> : rope_pairs_kernel<T, TT, kInterleaved>, grid, dim3(kRotThreads), 0, stream, p, items, far);
+    return launch_pdl(vectors ? rope_rows_kernel<T, TT, kInterleaved> : rope_pairs_kernel<T, TT, kInterleaved>, grid, dim3(kRotThreads), 0, stream, p, items);
 }
 
 }  // namespace ipotk
