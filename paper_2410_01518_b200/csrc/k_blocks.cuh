@@ -80,8 +80,8 @@ block_bounds_kernel(const T *__restrict__ K, T *__restrict__ lo, T *__restrict__
     }
 }
 
-// An append that takes the bounds along: a thread block copies a block's new rows, keys and values, and widens (or begins) its bounds by the
-// keys on their way through.  grid (blocks that rows [first_row, first_row + n) touch, units); srcK, srcV [units][n][d].  Bound: HBM, the copy.
+// An append that takes the bounds along: a thread block copies a block's new rows, keys and values, and bounds them by the keys on their way through, and with them the rows that were
+// there.  (Those are read again: their bounds may be those of an earlier replay of the same call, over rows that this one replaces.)  grid (blocks that rows [first_row, first_row + n) touch, units); srcK, srcV [units][n][d].  Bound: HBM, the copy.
 // kEarly as in append_kernel.
 template <typename T, bool kEarly>
 __global__ void __launch_bounds__(kBoundThreads)
@@ -96,7 +96,7 @@ append_bounds_kernel(const T *__restrict__ srcK, const T *__restrict__ srcV, T *
     __shared__ Vec part[2][kBoundThreads];
     const int vecs = d / Vec::kElems, r0 = threadIdx.x / vecs, v = threadIdx.x - r0 * vecs;
     const int block = first_row / rows_per_block + blockIdx.x, from = max(first_row, block * rows_per_block), to = min(first_row + n, (block + 1) * rows_per_block);
-    const int rows = to - from, side = min(kBoundThreads / vecs, rows);
+    const int rows = to - from, old = from - block * rows_per_block, side = min(kBoundThreads / vecs, max(rows, old));
     const size_t s = ((size_t)blockIdx.y * n + from - first_row) * vecs, t = ((size_t)blockIdx.y * unit_rows + from) * vecs;
     const Vec *sk = reinterpret_cast<const Vec *>(srcK) + s, *sv = reinterpret_cast<const Vec *>(srcV) + s;
     Vec *tk = reinterpret_cast<Vec *>(potK) + t, *tv = reinterpret_cast<Vec *>(potV) + t;
@@ -120,14 +120,21 @@ append_bounds_kernel(const T *__restrict__ srcK, const T *__restrict__ srcV, T *
                     widen(a, b, x[i], x[i]);
                 }
         }
+        const Vec *there = tk - (size_t)old * vecs;
+        for (int r = r0; r < old; r += RB * side) {
+            Vec x[RB];
+#pragma unroll
+            for (int i = 0; i < RB; ++i) x[i] = there[(size_t)min(r + i * side, old - 1) * vecs + v];   // (the last row again: it changes no bound)
+            if (r == r0 && r0 >= rows) a = b = x[0];
+#pragma unroll
+            for (int i = 0; i < RB; ++i) widen(a, b, x[i], x[i]);
+        }
     }
     join_bounds(a, b, part, side, vecs, r0, v);
     if (r0 == 0) {
         const size_t at = ((size_t)blockIdx.y * unit_blocks + block) * vecs + v;
-        Vec *l = reinterpret_cast<Vec *>(lo) + at, *h = reinterpret_cast<Vec *>(hi) + at;
-        if (from > block * rows_per_block) widen(a, b, *l, *h);   // rows that were there
-        *l = a;
-        *h = b;
+        reinterpret_cast<Vec *>(lo)[at] = a;
+        reinterpret_cast<Vec *>(hi)[at] = b;
     }
 }
 
