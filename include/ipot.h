@@ -413,7 +413,8 @@ int ipot_chunk_attention(ipot_t *pot, int layer, int n_layers, int n_tokens, con
  * its rows - so they are current for rows [0, len) whenever a call has returned (in stream order).
  * ipot_enable_blocks may be called at any time (rows that are in the pot are taken in at once); calling it again with another block_rows
  * starts anew, with the same one it does nothing.  The first call and such a change synchronise the stream and allocate
- * 2 * ceil(pot_size / block_rows) rows per unit.  ipot_enable_rope has to come before it (IPOT_E_STATE there otherwise).  block_rows: 16, 32, 64 or 128.
+ * 2 * ceil(pot_size / block_rows) rows per unit; they must not be captured, and calls that were captured before must not be
+ * replayed after them.  ipot_enable_rope has to come before it (IPOT_E_STATE there otherwise).  block_rows: 16, 32, 64 or 128.
  * Errors: INVALID, NOMEM, CUDA.
  */
 int ipot_enable_blocks(ipot_t *pot, int block_rows);

@@ -3,8 +3,8 @@
 //
 // rope_table_kernel: entry (p, i) is the cosine (sine) of p * f_i times a magnitude.  Far positions need more than fp32: the
 //   angle is taken in turns, p * (f_i / 2 pi), in 64 bits, its whole turns are dropped there (exact), and cosine and sine of
-//   what is left, at most half a turn, are fp32, rounded once more where the table is bf16.  Error of the angle: 2^-52 of it (the two roundings of
-//   the product) + 2^-24 of half a turn.
+//   what is left, at most half a turn, are fp32, rounded once more where the table is bf16.  Error of the angle: up to
+//   (ln b + 8) 2^-53 of it, b the base - the exponent of b is rounded, and so are the power, the stretched base or the blend, 2 pi, the quotient and the product - + 2^-24 of half a turn.
 // rope_rows_kernel: lo' = fma(lo, cos, -(hi * sin)), hi' = fma(hi, cos, lo * sin), as the movers have it, in fp32, rounded once to the
 //   rows' type; channels behind the rotated part are copied.  A thread has one 16-byte vector (half pairing: a vector and its
 //   partners) of kRowHeads heads of a token: the table's vectors are loaded once for them.  Bound: HBM, every row in and out.
@@ -113,7 +113,7 @@ struct RowHeads {
 // grid (blocks over tokens x items, head groups, layers x streams).  Items of a row: half pairing, one per vector of the lower
 // half (it brings its partner); interleaved, one per rotated vector; and one per vector, or two vectors, that are copied.  Both kinds load before
 // and store behind the rotation: a warp has items of both.  16 streams x 2048 tokens x 40 heads x 128 channels (671 MB): 98.8 us, 6.8 TB/s, all or half of them rotated; streams of
-// different lengths, half as many rows, 60 us, 5.9 TB/s.  (Stored as a struct of elements: 138 us.  Stores that are evicted first: no gain out of place, 84 MB in place 20 -> 24 us.)
+// different lengths, half as many rows, 58.5 us, 6.1 TB/s.  (Stored as a struct of elements: 138 us.  Stores that are evicted first: no gain out of place, 84 MB in place 20 -> 24 us.)
 template <typename T, typename TT, bool kInterleaved>
 __global__ void __launch_bounds__(kRotThreads)
 rope_rows_kernel(const __grid_constant__ RopeRowsParams p, int items)

@@ -24,8 +24,8 @@ def test_a_ramp_that_does_not_stretch_has_magnitude_one(factor, dtype):
     ang = np.arange(n, dtype=np.longdouble)[:, None] * f[None]
     for got, want in ((cos, np.cos(ang)), (sin, np.sin(ang))):
         g, w = got.double().cpu().numpy(), (want * mag).astype(np.float64)
-        # the frequency itself is off by a few 2^-53 (pow, the division by 2 pi, the blend); 2^-50 of the angle covers them and the product
-        bound = mag * (2.0 ** -50 * ang.astype(np.float64) + math.pi * 2.0 ** -25 + 2.0 ** -23 + 2.0 ** -24) + half_step * np.abs(w) + 2.0 ** -130
+        # the frequency's own roundings (exponent, power, 2 pi, quotient, blend) and the product's: (ln base + 8) 2^-53 < 2^-48 of the angle
+        bound = mag * (2.0 ** -48 * ang.astype(np.float64) + math.pi * 2.0 ** -25 + 2.0 ** -23 + 2.0 ** -24) + half_step * np.abs(w) + 2.0 ** -130
         assert (np.abs(g - w) <= bound).all(), float(np.max(np.abs(g - w) / bound))
 
 
