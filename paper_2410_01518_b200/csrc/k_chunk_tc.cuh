@@ -7,7 +7,7 @@
 //   softmax     a thread owns half of a row (one warp per scheduler and stream would be a chain of latencies: 1900 cycles a tile, two 1500): p = 2^(s c - m - 40),
 //               l += p in fp32, and p as bf16 over S in tensor memory.  No maximum is taken: fp32 and bf16 have the same exponents, so p is as exact far above 1
 //               as below.  The reference m is 0 unless the sum of the row's first tile is far from 1, and only a later tile whose sum passes 2^24 moves it (the row's sums and output
-//               are then scaled down).  The 40 orders are what a row's weights can sum up to so: all p together stay below 1, and no sum of p v on the way is larger than the largest value.  Tiles with columns that some row does not see, those two kinds, and those of a row whose reference is beyond 2^24, take a general form that does take the maximum.  All exponentials are the
+//               are then scaled down).  The 40 orders are what a row's weights can sum up to so: all p together stay below 1, and no sum of p v on the way is larger than the largest value.  Tiles with columns that some row does not see, those two kinds, and those of a row whose reference is beyond 2^12, take a general form that does take the maximum.  All exponentials are the
 //               special-function unit's: a quarter of them as a polynomial on the FMA pipe took 1016 us for 4 streams x 2048 tokens over 6144 rows instead of 950
 //               (in long runs the power limit holds the clock at 1.6 GHz, and what is issued costs power).
 //   O += P V    P from tensor memory, V as it lies (channels contiguous: the N-major operand layout), 128 x D fp32 in tensor memory
@@ -39,11 +39,12 @@ constexpr unsigned long long kChunkLandNs = 200ull * 1000 * 1000;
 constexpr float kChunkLift = 40.f, kChunkLifted = 1099511627776.f;   // and 2^40
 constexpr float kChunkMost = 1.52587890625e-05f;                     // 2^24 2^-40
 constexpr float kChunkLeast = 2.220446049250313e-16f;                // 2^-12 2^-40
-// A reference is a rounded product, and s c, not rounded before the reference is subtracted, misses it by up to half its last place: 1 and more from 2^24 on, further out more than the
-// exponential's range.  The general form rounds the product, so that the row's maximum comes out as exactly 0; near 0 that is as good.  References up to here are whole numbers, which add up exactly.  From here on a row takes nothing but the general form: its reference
-// then waits in its threads' shared memory and is NaN in their registers, so that a plain tile's sum is NaN and the check that there is fails.  (4 streams x 2048 tokens over 6144 rows
-// 953.4 -> 954.4 us, 2048 tokens into an empty pot 45.0 -> 45.6; a compare per tile and a flag across them cost 4.5 %.)
-constexpr float kChunkFar = 16777216.f;       // 2^24
+// The row's maximum is a rounded product, and s c, not rounded before the reference is subtracted, misses it by up to half its last place: 1 from 2^24 on, further out more than the exponential's
+// range.  The general form rounds the product, so that the maximum comes out as what it was taken for.  Up to here that differs from a plain tile's weights by 2^-13 of an order at most, and references
+// are whole numbers, which add up exactly.  From here on a row takes nothing but the general form: its reference then waits in its threads' shared memory and is NaN in their registers, so that a
+// plain tile's sum is NaN and the check that there is fails.  (4 streams x 2048 tokens over 6144 rows 953.4 -> 954.4 us, 2048 tokens into an empty pot 45.0 -> 45.6; a compare per tile and a
+// flag across them cost 4.5 %.)
+constexpr float kChunkFar = 4096.f;
 
 template <int D, bool kSplit> struct ChunkTc {
     static constexpr int kStreams = D > 128 ? 1 : 2;

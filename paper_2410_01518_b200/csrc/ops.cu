@@ -28,7 +28,7 @@ cudaError_t launch_rope_rows(const RopeRowsParams &p, bool f32, bool table_f32, 
 }
 
 // Few rows have a kernel of their own: up to 8 of a KV head, or two groups of 8 that each go over the keys.
-// Two groups (us, this / the other kernel for 9 rows and more; 16 rows, units x keys).  bf16: as long as half of L2 holds the keys, so that the second group finds what the first has read, and
+// Two groups (us, this / the other kernel for 9 rows and more, or how many times as long the other takes; 16 rows, units x keys).  bf16: as long as half of L2 holds the keys, so that the second group finds what the first has read, and
 // the groups do not queue for SMs (a block's shared memory goes with d); or where a handful of units leaves the other kernel, 8 blocks a unit, most SMs idle.
 //   d = 64   16 x 2000 6.3/8.8   64 x 4095 20/21    128 x 2000 21/19   256 x 2000 40/38
 //   d = 128  4 x 32000 29/40   8 x 4095 14/15   8 x 16000 28/25   32 x 2000 12/15   32 x 16000 57/52   64 x 500 10/12   64 x 8000 57/53   128 x 500 17/12   256 x 4095 153/96

@@ -114,3 +114,26 @@ def test_values_up_to_two_to_the_127_over_selected_blocks(logit, dtype):
         assert bool(((lse[0, 0].double() - e).abs() <= 2 * dx + 2.0 ** -20 + N * 2.0 ** -24 + 2.0 ** -22 * e.abs()).all())
     finally:
         c.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,length,n", [(64, 700, 200), (128, 700, 200), (64, 100, 1500)])
+@pytest.mark.parametrize("power,below", [(24, b) for b in (-3, 0, 1, 2, 3, 17, 38, 39, 64, 65, 66, 104, 105)] + [(12, b) for b in (-3, 0, 1, 2, 39, 40, 41)] + [(p, 1) for p in (10, 11, 13, 16, 20, 22)])
+def test_references_far_from_zero(power, below, d, length, n):
+    """All logits equal and 2^power - below - 1/2 in binary orders: whatever form a tile takes, every key weighs the same."""
+    c = Case("bf16", 1, 1, 4, 2, d, length, n)
+    try:
+        orders = 1.4426950408889634 / math.sqrt(d)   # of a unit of q . k (the kernel's own differs in the eighth digit: at 2^24 by less than 2)
+        whole = round((2.0 ** power - below - 0.5) / orders)
+        for i in range(4):   # the number in base 256, a digit a channel
+            for x in (c.K, c.k):
+                x[..., i] = (whole >> 8 * i) & 255
+            c.q[..., i] = 2.0 ** (8 * i)
+        for x in (c.K, c.k, c.q):
+            x[..., 4:] = 0
+        ipot.ipot_reset(c.h)
+        ipot.ipot_append_chunk(c.h, c.K, c.V, length)
+        c.run()
+        check_exact_logits(c)
+    finally:
+        c.close()
